@@ -1,0 +1,578 @@
+"""Performance cases of the beam-search operators: selection, the paged cache's page operations and its attention.
+
+  op "select"   one step of beam search's selection over beams and vocabulary (pdec.beam_select):
+                log-softmax of every live beam's logits, the K best extensions of a sentence;
+  op "attend"   one decoding step of attention over a paged key/value cache in float32, bfloat16 or
+                4 bits (PagedCache.attend), with the step's own token appended first where "append" is
+                set; the beams of a sentence share the pages of their common prefix;
+  op "fork"     the cache follows the selected beams (PagedCache.fork): page tables gathered by parent,
+                shared pages counted, half-filled shared pages copied, pages for the next token found;
+  op "compact"  the pages in use move to the front of the pool (PagedCache.compact).
+
+Layouts (the cache's documented format):
+  K  [layers][pages][kv heads][page_size][head_dim],  V  [layers][pages][kv heads][head_dim][page_size];
+  4 bits: along the last axis, words of eight values; value e of a word lies at bits 4 (e // 2 + 4 (e % 2));
+  k_scale, v_scale [layers][pages][kv heads][page_size][groups][2] bfloat16: (step, least value) of each group of
+  min(head_dim, 32) dimensions of a token's head vector.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+if own:
+    from paper_2305_10427_amd import pdec
+
+
+# --- cases ---------------------------------------------------------------------
+
+
+def _select(name, B, K, V, dtype, alpha, finished):
+    return {"name": name, "op": "select", "B": B, "K": K, "V": V, "dtype": dtype, "alpha": alpha, "finished": finished}
+
+
+def _attend(name, cache, B, K, heads, kv_heads, dh, lo, hi, ps, shared, append, out):
+    return {"name": name, "op": "attend", "cache": cache, "B": B, "K": K, "heads": heads, "kv_heads": kv_heads,
+            "dh": dh, "lo": lo, "hi": hi, "ps": ps, "shared": shared, "append": append, "out": out}
+
+
+def _pages(name, op, cache, layers, B, K, kv_heads, dh, lo, hi, ps, shared, spare):
+    return {"name": name, "op": op, "cache": cache, "layers": layers, "B": B, "K": K, "kv_heads": kv_heads, "dh": dh,
+            "lo": lo, "hi": hi, "ps": ps, "shared": shared, "spare": spare}
+
+
+def listed():
+    return [
+        # the smallest selection: one sentence of the tiny model, four beams; launch latency
+        _select("select_tiny", 1, 4, 1000, "f32", 1.0, 0.0),
+        # interactive translation of one sentence, Transformer-base vocabulary, the usual five beams
+        _select("select_base_b1", 1, 5, 58101, "f32", 0.6, 0.0),
+        # offline translation in batches of 64, a fifth of the hypotheses finished
+        _select("select_base_b64", 64, 5, 58101, "f32", 0.6, 0.2),
+        # the large multilingual vocabulary, batch 32, bfloat16 logits
+        _select("select_large_b32_bf16", 32, 4, 250027, "bf16", 1.0, 0.1),
+        # the smallest attention: four beams of one short sentence, float32
+        _attend("attend_tiny_f32", "f32", 1, 4, 4, 4, 16, 16, 16, 16, 0.5, True, "f32"),
+        # a layer of a decoding step, Transformer-base shape, 64 sentences of mixed length, five beams each
+        _attend("attend_base_b64_bf16", "bf16", 64, 5, 8, 8, 64, 15, 138, 16, 0.7, True, "bf16"),
+        # the large shape, batch 32, the cache held in 4 bits
+        _attend("attend_large_b32_int4", "int4", 32, 5, 16, 16, 64, 30, 256, 16, 0.7, True, "bf16"),
+        # two long documents, grouped heads, 4 bits: a long axis and few rows
+        _attend("attend_long_int4", "int4", 2, 4, 16, 4, 128, 20011, 32749, 64, 0.9, False, "f32"),
+        # greedy rows with long caches of their own (nothing shared): the largest attention
+        _attend("attend_long_bf16", "bf16", 16, 1, 16, 16, 64, 8191, 16381, 32, 0.0, False, "bf16"),
+        # the cache follows the beams after a selection: Transformer-base, batch 64, float32, all layers
+        _pages("fork_base_b64", "fork", "f32", 6, 64, 5, 8, 64, 15, 138, 16, 0.7, 1.5),
+        # the large shape, batch 32, bfloat16, all twelve layers
+        _pages("fork_large_b32", "fork", "bf16", 12, 32, 5, 16, 64, 30, 256, 16, 0.7, 1.5),
+        # a pool in 4 bits, half of it free and scattered, is moved together
+        _pages("compact_large_b32", "compact", "int4", 12, 32, 5, 16, 64, 30, 256, 16, 0.7, 2.0),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(["select", "select", "attend", "attend", "attend", "fork", "compact"])
+    while True:
+        if op == "select":
+            B, K = _log_int(rng, 1, 64), rng.choice([1, 2, 3, 4, 5, 5, 6, 8, 10, 13, 16])
+            c = _select("", B, K, _log_int(rng, 1000, 250027), rng.choice(["f32", "bf16"]),
+                        rng.choice([0.0, 0.6, 1.0]), rng.choice([0.0, 0.1, 0.3]))
+            fits = B * K * c["V"] <= 18_000_000
+        elif op == "attend":
+            long = rng.random() < 0.3
+            kv, per, dh = rng.choice([4, 8, 16]), rng.choice([1, 1, 1, 2, 4]), rng.choice([16, 32, 64, 64, 128])
+            hi = _log_int(rng, 1024, 32749) if long else _log_int(rng, 1, 1024)
+            lo = rng.randint(max(1, hi // 6), hi)
+            B, K = _log_int(rng, 1, 16 if long else 64), rng.choice([1, 2, 4, 5, 5, 8, 16])
+            cache = rng.choice(["f32", "bf16", "bf16", "int4", "int4"])
+            c = _attend("", cache, B, K, kv * per, kv, dh, lo, hi, rng.choice([16, 32, 64, 128]),
+                        rng.choice([0.0, 0.5, 0.8]), rng.random() < 0.7, rng.choice(["f32", "bf16"]))
+            fits = B * K * hi * kv * dh <= (100_000_000 if cache == "f32" else 200_000_000)
+        else:
+            kv, dh = rng.choice([4, 8, 16]), rng.choice([16, 32, 64, 128])
+            hi = _log_int(rng, 4, 512)
+            lo = rng.randint(max(1, hi // 6), hi)
+            c = _pages("", op, rng.choice(["f32", "bf16", "int4"]), rng.randint(1, 12), _log_int(rng, 1, 64),
+                       rng.choice([1, 2, 4, 5, 8]), kv, dh, lo, hi, rng.choice([16, 32, 64]),
+                       rng.choice([0.0, 0.5, 0.8]), rng.choice([1.3, 2.0]))
+            fits = c["layers"] * _tokens(c) * kv * dh <= 250_000_000
+        if fits:
+            del c["name"]
+            return c
+
+
+# --- what a case's numbers say --------------------------------------------------
+
+
+def _spread(case):
+    """Length of each sentence: spread evenly over [lo, hi]."""
+    B = case["B"]
+    return [case["hi"] if B == 1 else case["lo"] + (case["hi"] - case["lo"]) * b // (B - 1) for b in range(B)]
+
+
+def _shared_pages(case, n):
+    """Full pages that all beams of a sentence of n tokens share."""
+    return int(n * case["shared"]) // case["ps"] if case["K"] > 1 else 0
+
+
+def _tokens(case):
+    """Tokens in the pages in use, every page whole and counted once."""
+    ps = case["ps"]
+    return sum(ps * (_shared_pages(case, n) + case["K"] * (-(-n // ps) - _shared_pages(case, n))) for n in _spread(case))
+
+
+def _groups(dh):
+    return max(1, dh // 32)
+
+
+def _token_bytes(case):
+    """Bytes of a token's key and value in one layer."""
+    dh = case["dh"]
+    return case["kv_heads"] * {"f32": 8 * dh, "bf16": 4 * dh, "int4": dh + 8 * _groups(dh)}[case["cache"]]
+
+
+def _parents(case):
+    """Distinct parents that survive a step, of K beams."""
+    return (case["K"] + 1) // 2
+
+
+def work(case):
+    B, K = case["B"], case["K"]
+    if case["op"] == "select":
+        live = B * K - int(B * K * case["finished"])
+        n = live * case["V"]
+        return {"bytes": n * (4 if case["dtype"] == "f32" else 2) + B * K * 40, "flops": 4 * n}
+    S, ns = B * K, _spread(case)
+    tables = S * 4 * (-(-(case["hi"] + 1) // case["ps"]) + 2)
+    if case["op"] == "attend":
+        tok = sum(_shared_pages(case, n) * case["ps"] + K * (n - _shared_pages(case, n) * case["ps"]) for n in ns)
+        rows = S * case["heads"] * case["dh"]
+        new = S * 3 * _token_bytes(case) if case["append"] else 0
+        return {"bytes": tok * _token_bytes(case) + rows * (4 + (4 if case["out"] == "f32" else 2)) + tables + new,
+                "flops": 4 * case["heads"] * case["dh"] * K * sum(ns)}
+    page = case["layers"] * case["ps"] * _token_bytes(case)
+    if case["op"] == "fork":
+        moved = sum(K - _parents(case) for n in ns if n % case["ps"])
+    else:       # of a pool of spare times the pages in use, the used pages are spread evenly
+        used = _tokens(case) // case["ps"]
+        moved = int(used * (1 - used / _pool_pages(case)))
+    return {"bytes": 2 * moved * page + 2 * tables + 4 * _pool_pages(case), "flops": 0}
+
+
+def _pool_pages(case):
+    return int(_tokens(case) // case["ps"] * case.get("spare", 1.25)) + case["B"] * case["K"] + 1
+
+
+# --- inputs ----------------------------------------------------------------------
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(7919 * seed + 17)
+    rng = np.random.default_rng(seed)
+    return _prepare_select(case, g, rng) if case["op"] == "select" else _prepare_cache(case, g, rng)
+
+
+def _prepare_select(case, g, rng):
+    B, K, V = case["B"], case["K"], case["V"]
+    # logits of the framework's models have a standard deviation of about 3
+    x = torch.randn((B, K, V), generator=g, device="cuda") * 3.0
+    done = np.zeros(B * K, np.int32)
+    done[rng.permutation(B * K)[:int(B * K * case["finished"])]] = 1
+    step = 12
+    lens = np.where(done, rng.integers(2, step + 1, B * K), step).astype(np.int32)
+    scores = (-1.3 * lens - rng.random(B * K) * 4).astype(np.float32)
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a).reshape(B, K)).cuda()  # noqa: E731
+    limit = torch.from_numpy(rng.integers(step + 1, 4 * step, B).astype(np.int32)).cuda()
+    return {"case": case, "logits": x if case["dtype"] == "f32" else x.to(torch.bfloat16), "scores": dev(scores),
+            "lens": dev(lens), "done": dev(done), "limit": limit}
+
+
+def _tables(case, rng):
+    """Page table [S][pages per sequence] (-1: none), the pages scattered over the pool, and the lengths."""
+    K, ps = case["K"], case["ps"]
+    ns = _spread(case)
+    P = _pool_pages(case)
+    ids = rng.permutation(P)[:_tokens(case) // ps]
+    ld = -(-(case["hi"] + 1) // ps)
+    table = np.full((len(ns) * K, ld), -1, np.int32)
+    at = 0
+    for b, n in enumerate(ns):
+        sh, all_ = _shared_pages(case, n), -(-n // ps)
+        table[b * K:(b + 1) * K, :sh] = ids[at:at + sh]
+        at += sh
+        for k in range(K):
+            table[b * K + k, sh:all_] = ids[at:at + all_ - sh]
+            at += all_ - sh
+    return table, np.repeat(np.asarray(ns, np.int32), K), P
+
+
+def _prepare_cache(case, g, rng):
+    table, lens, P = _tables(case, rng)
+    L, H, ps, dh = case.get("layers", 1), case["kv_heads"], case["ps"], case["dh"]
+    S = len(lens)
+    st = {"case": case, "table": torch.from_numpy(table).cuda(), "lens": torch.from_numpy(lens).cuda(),
+          "last": torch.from_numpy(lens - 1).cuda()}
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    if case["cache"] == "int4":
+        st["k"] = torch.randint(0, 256, (L, P, H, ps, dh // 2), generator=g, device="cuda", dtype=torch.uint8)
+        st["v"] = torch.randint(0, 256, (L, P, H, dh, ps // 2), generator=g, device="cuda", dtype=torch.uint8)
+        for n in ("k_scale", "v_scale"):   # groups of values in about [-2, 2]
+            step = 0.2 + 0.15 * torch.rand((L, P, H, ps, _groups(dh)), generator=g, device="cuda")
+            least = -7.5 * step + 0.3 * rnd(*step.shape)
+            st[n] = torch.stack([step, least], -1).to(torch.bfloat16)
+    else:
+        t = torch.float32 if case["cache"] == "f32" else torch.bfloat16
+        st["k"] = torch.empty((L, P, H, ps, dh), dtype=t, device="cuda").normal_(generator=g)
+        st["v"] = torch.empty((L, P, H, dh, ps), dtype=t, device="cuda").normal_(generator=g)
+    if case["op"] == "attend":
+        st["q"] = 2.0 * rnd(S, case["heads"], dh)
+        if case["append"]:
+            t = torch.float32 if case["cache"] == "f32" else torch.bfloat16
+            st["new_k"], st["new_v"] = rnd(S, H, dh).to(t), rnd(S, H, dh).to(t)
+    elif case["op"] == "fork":
+        K = case["K"]
+        par = np.empty(S, np.int32)
+        for b in range(case["B"]):   # every survivor has a child, the others are children of any of them
+            alive = rng.permutation(K)[:_parents(case)]
+            par[b * K:(b + 1) * K] = b * K + rng.permutation(np.concatenate([alive, rng.choice(alive, K - len(alive))]))
+        st["parents"] = torch.from_numpy(par).cuda()
+    return st
+
+
+def _cache(st):
+    """The cache object that a program keeps beside its tensors."""
+    if "handle" not in st:
+        c = st["case"]
+        st["handle"] = pdec.PagedCache(c["cache"], c.get("layers", 1), st["k"].shape[1], c["ps"], c["kv_heads"], c["dh"],
+                                       k=st["k"], v=st["v"], k_scale=st.get("k_scale"), v_scale=st.get("v_scale"))
+    return st["handle"]
+
+
+# --- one pass ----------------------------------------------------------------------
+
+EOS, PAD = 2, 0
+
+
+def run(st):
+    c = st["case"]
+    if c["op"] == "select":
+        return _run_select(st)
+    if c["op"] == "attend":
+        return _run_attend(st)
+    return _run_fork(st) if c["op"] == "fork" else _run_compact(st)
+
+
+def _run_select(st):
+    c = st["case"]
+    if own:
+        r = pdec.beam_select(st["logits"], st["scores"], st["lens"], st["done"], eos_id=EOS, pad_id=PAD,
+                             alpha=c["alpha"], max_len=st["limit"])
+        return {"scores": r.scores, "parents": r.parents, "tokens": r.tokens, "lens": r.lens, "done": r.done, "src": r.src,
+                "flags": r.flags}
+    # keys are compared with each other across rows: 64 bits, or near keys change places
+    B, K, V = c["B"], c["K"], c["V"]
+    n = min(K, V)
+    x = st["logits"].float()
+    bad = torch.isnan(x) | (x == math.inf)
+    x = torch.where(bad, -math.inf, x)
+    # the n best words of each row, equal logits in word order: unique 64-bit keys of (logit, word)
+    bits = (x + 0.0).view(torch.int32).to(torch.int64)
+    order = torch.where(bits < 0, -(bits & 0x7FFFFFFF), bits)
+    _, word = torch.topk(order * (1 << 20) - torch.arange(V, device=x.device), n, dim=-1)
+    top = torch.gather(x, 2, word).double()
+    most = x.amax(-1, keepdim=True).double()
+    lse = most + torch.exp(x.double() - most).sum(-1, keepdim=True).log()
+    s = st["scores"].double()[:, :, None]
+    fin = (st["done"] != 0)[:, :, None]
+    live = torch.isfinite(s)
+    first = torch.arange(n, device=x.device) == 0
+    cum = torch.where(fin, s, s + (top - lse))
+    cum = torch.where(live & (~fin | first) & torch.isfinite(cum), cum, -math.inf)
+    m = st["lens"][:, :, None] + torch.where(fin, 0, 1)
+    key = (cum / m.double().clamp(min=1).pow(c["alpha"])).reshape(B, K * n)
+    _, at = torch.sort(key, dim=-1, descending=True, stable=True)
+    at = at[:, :K]
+    pick = lambda t: torch.gather(t.expand(B, K, n).reshape(B, K * n), 1, at)  # noqa: E731
+    cum = pick(cum)
+    there = cum > -math.inf
+    par = torch.where(there, at // n, -1)
+    tok = torch.where(there, pick(torch.where(fin, PAD, word)), PAD)
+    m = torch.where(there, pick(m), 0)
+    done = ~there | pick(fin) | (tok == EOS) | (m >= st["limit"][:, None])
+    src = torch.where(done, -1, par + K * torch.arange(B, device=x.device)[:, None])
+    i32 = lambda t: t.to(torch.int32)  # noqa: E731
+    flags = 8 * (bad.any(-1) & live[..., 0] & ~fin[..., 0]).any(-1)
+    return {"scores": cum.float(), "parents": i32(par), "tokens": i32(tok), "lens": i32(m), "done": i32(done),
+            "src": i32(src), "flags": i32(flags)}
+
+
+_NIB = [0, 4, 1, 5, 2, 6, 3, 7]      # nibble of value e of a word
+_VAL = [0, 2, 4, 6, 1, 3, 5, 7]      # value in nibble n of a word
+
+
+def _unpack(b):
+    """Codes of packed bytes, eight a word along the last axis, as float32."""
+    n = torch.stack([b & 15, b >> 4], -1).reshape(*b.shape[:-1], -1, 8)
+    return n[..., _NIB].reshape(*b.shape[:-1], -1).float()
+
+
+def _quantise(x):
+    """Codes and (step, least value) of groups of min(dh, 32) values along the last axis."""
+    S, H, dh = x.shape
+    x = x.float().reshape(S, H, _groups(dh), -1)
+    lo, hi = x.amin(-1), x.amax(-1)
+    least = _bf16_down(lo)
+    # the smallest bfloat16 step with 15 step >= hi - least, tested by an exact product (on halves: no overflow)
+    half = hi * 0.5 - least * 0.5
+    step = _bf16_down(half * (2 / 15))
+    step = torch.where(step * 7.5 < half, (step.view(torch.int32) + 0x10000).view(torch.float32), step)
+    code = torch.where(step[..., None] > 0, torch.round((x - least[..., None]) / step[..., None]), 0.0).clamp(0, 15)
+    return code.to(torch.uint8).reshape(S, H, dh), torch.stack([step, least], -1).to(torch.bfloat16)
+
+
+def _bf16_down(x):
+    """The largest bfloat16 up to x, as float32."""
+    u = x.view(torch.int32)
+    low = u & 0xFFFF
+    return (u - low + torch.where((low != 0) & (x < 0), 0x10000, 0).to(torch.int32)).view(torch.float32)
+
+
+def _values(st, layer, pages):
+    """Keys and values of pages [S][n] of a layer as float32 [S][kv heads][n page_size][dh]."""
+    c = st["case"]
+    H, ps, dh = c["kv_heads"], c["ps"], c["dh"]
+    S, n = pages.shape
+    k, v = st["k"][layer][pages], st["v"][layer][pages]
+    if c["cache"] == "int4":
+        k, v = _unpack(k), _unpack(v)
+    k, v = k.float(), v.float().transpose(-1, -2)
+    if c["cache"] == "int4":
+        G = _groups(dh)
+        for t, p in ((k, "k_scale"), (v, "v_scale")):
+            f = st[p][layer][pages].float()
+            t = t.unflatten(-1, (G, -1))
+            t.mul_(f[..., 0][..., None]).add_(f[..., 1][..., None])
+    flat = lambda t: t.permute(0, 2, 1, 3, 4).reshape(S, H, n * ps, dh)  # noqa: E731
+    return flat(k), flat(v)
+
+
+def _append(st):
+    """Writes the step's own token into its page of layer 0, at position len - 1."""
+    c = st["case"]
+    ps, last = c["ps"], st["last"].long()
+    page = torch.gather(st["table"].long(), 1, (last // ps)[:, None])[:, 0]
+    slot = last % ps
+    if c["cache"] != "int4":
+        st["k"][0][page, :, slot] = st["new_k"]
+        st["v"][0][page, :, :, slot] = st["new_v"]
+        return
+    for name, new in (("k", st["new_k"]), ("v", st["new_v"])):
+        code, par = _quantise(new)
+        st[name + "_scale"][0][page, :, slot] = par
+        if name == "k":
+            n = code.unflatten(-1, (-1, 8))[..., _VAL].reshape(*code.shape[:2], -1, 2)
+            st["k"][0][page, :, slot] = n[..., 0] | (n[..., 1] << 4)
+        else:
+            nib = torch.tensor(_NIB, device=slot.device)[slot % 8]
+            byte, shift = slot // 8 * 4 + nib // 2, (4 * (nib % 2))[:, None, None]
+            old = st["v"][0][page, :, :, byte]
+            st["v"][0][page, :, :, byte] = ((old & ~(15 << shift)) | (code.long() << shift)).to(torch.uint8)
+
+
+def _run_attend(st):
+    c = st["case"]
+    t = torch.float32 if c["out"] == "f32" else torch.bfloat16
+    if own:
+        o = _cache(st).attend(st["q"], st["table"], st["lens"], group=c["K"], max_len=c["hi"], new_k=st.get("new_k"),
+                              new_v=st.get("new_v"), out_dtype=t)
+        if not c["append"]:
+            return {"out": o}
+        if c["cache"] != "int4":
+            return {"out": o, "k": st["k"], "v": st["v"]}
+        k, v = _cache(st).read(st["table"], st["lens"], st["last"])
+        return {"out": o, "k": k[:, 0], "v": v[:, 0]}
+    if c["append"]:
+        _append(st)
+    S, H, dh = c["B"] * c["K"], c["kv_heads"], c["dh"]
+    k, v = _values(st, 0, st["table"].clamp(min=0))
+    q = st["q"].reshape(S, H, -1, dh)
+    w = torch.matmul(q, k.transpose(-1, -2)) / math.sqrt(dh)
+    w = w.masked_fill((torch.arange(k.shape[2], device=q.device) >= st["lens"][:, None])[:, None, None], -math.inf)
+    w = torch.exp(w - w.amax(-1, keepdim=True))
+    o = (torch.matmul(w, v) / w.sum(-1, keepdim=True)).reshape(S, c["heads"], dh).to(t)
+    if not c["append"]:
+        return {"out": o}
+    if c["cache"] != "int4":
+        return {"out": o, "k": st["k"], "v": st["v"]}
+    last = st["last"].long()[:, None, None, None].expand(S, H, 1, dh)
+    return {"out": o, "k": torch.gather(k, 2, last)[:, :, 0], "v": torch.gather(v, 2, last)[:, :, 0]}
+
+
+def _pools(st):
+    return {n: st[n] for n in ("k", "v", "k_scale", "v_scale") if n in st}
+
+
+def _count(pages, P):
+    return torch.zeros(P + 1, dtype=torch.int64, device=pages.device).scatter_add_(
+        0, torch.where(pages < 0, P, pages).reshape(-1), torch.ones_like(pages).reshape(-1))[:P]
+
+
+def _run_fork(st):
+    c = st["case"]
+    if own:
+        r = _cache(st).fork(st["table"], st["lens"], st["parents"], grow=True)
+        return {"table": r.table, "lens": r.lens, "refs": r.refs, "status": r.status} | _pools(st)
+    ps, P = c["ps"], st["k"].shape[1]
+    par = st["parents"].long()
+    dev = par.device
+    at = par.clamp(min=0)
+    old = torch.where(par >= 0, st["lens"].long()[at], 0)
+    there = torch.arange(st["table"].shape[1], device=dev) * ps < old[:, None]
+    table = torch.where(there, st["table"].long()[at], -1)
+    refs = _count(table, P)
+    grow = par >= 0
+    s = torch.arange(len(par), device=dev)
+    half = grow & (old % ps != 0)
+    col = (old // ps)[:, None]
+    page = torch.where(half, torch.gather(table, 1, col)[:, 0], P)
+    ones = torch.ones_like(page)
+    writers = torch.zeros(P + 1, dtype=torch.int64, device=dev).scatter_add_(0, page, ones)
+    first = torch.full((P + 1,), len(par), device=dev).scatter_reduce_(0, page, s, "amin")
+    whole = torch.cat([refs, refs.new_zeros(1)])[page] == writers[page]
+    copy = half & ~(whole & (first[page] == s))
+    need = copy | (grow & ~half)
+    free = torch.sort((refs > 0).to(torch.int8), stable=True)[1]
+    new = free[(need.cumsum(0) - 1).clamp(min=0)]
+    table.scatter_(1, col, torch.where(need, new, torch.gather(table, 1, col)[:, 0])[:, None])
+    refs = _count(table, P)
+    src, dst = page[copy], new[copy]
+    for t in _pools(st).values():
+        t[:, dst] = t[:, src]
+    i32 = lambda t: t.to(torch.int32)  # noqa: E731
+    status = torch.stack([torch.zeros_like(refs[0]), (refs > 0).sum()])
+    return {"table": i32(table), "lens": i32(old + grow), "refs": i32(refs), "status": i32(status)} | _pools(st)
+
+
+def _run_compact(st):
+    c = st["case"]
+    if own:
+        r = _cache(st).compact(st["table"], st["lens"])
+        return {"table": r.table, "remap": r.remap, "status": r.status} | _pools(st)
+    ps, P = c["ps"], st["k"].shape[1]
+    table = st["table"].long()
+    dev = table.device
+    there = torch.arange(table.shape[1], device=dev) * ps < st["lens"].long()[:, None]
+    used = _count(torch.where(there, table, -1), P) > 0
+    n = used.sum()
+    ids = torch.arange(P, device=dev)
+    src, dst = ids[used & (ids >= n)], ids[~used & (ids < n)]
+    remap = torch.where(used, ids, -1)
+    remap[src] = dst
+    for t in _pools(st).values():
+        t[:, dst] = t[:, src]
+    out = torch.where(there, remap[table.clamp(min=0)], -1)
+    i32 = lambda t: t.to(torch.int32)  # noqa: E731
+    return {"table": i32(out), "remap": i32(remap), "status": torch.stack([torch.tensor(len(src), device=dev), n]).to(torch.int32)}\
+        | _pools(st)
+
+
+# --- the same in 64 bits, one sequence at a time -------------------------------------
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    if case["op"] == "select":
+        return _exact_select(case, st)
+    if case["op"] == "attend":
+        return _exact_attend(case, st)
+    return None
+
+
+def _exact_select(case, st):
+    B, K, V = case["B"], case["K"], case["V"]
+    sc, ln, dn = (st[n].cpu().numpy() for n in ("scores", "lens", "done"))
+    lim = st["limit"].cpu().numpy()
+    got = {n: np.zeros((B, K), np.int32) for n in ("parents", "tokens", "lens", "done", "src")}
+    scores = np.zeros((B, K))
+    for b in range(B):
+        cands = []
+        for k in range(K):
+            if dn[b, k]:
+                cands.append((-(float(sc[b, k]) / float(ln[b, k]) ** case["alpha"]), k, 0, float(sc[b, k]), PAD, int(ln[b, k]), True))
+                continue
+            x = st["logits"][b, k].double().cpu().numpy()
+            m = x.max()
+            lse = m + math.log(np.exp(x - m).sum())
+            best = np.lexsort((np.arange(V), -x))[:K] if V <= 4 * K else None
+            if best is None:
+                cut = np.partition(x, V - K)[V - K]
+                near = np.nonzero(x >= cut)[0]
+                best = near[np.lexsort((near, -x[near]))][:K]
+            for r, v in enumerate(best):
+                cum = float(sc[b, k]) + (x[v] - lse)
+                cands.append((-(cum / float(ln[b, k] + 1) ** case["alpha"]), k, r, cum, int(v), int(ln[b, k]) + 1, False))
+        cands.sort()
+        for j, (_, k, _, cum, v, n, fin) in enumerate(cands[:K]):
+            scores[b, j] = cum
+            got["parents"][b, j], got["tokens"][b, j], got["lens"][b, j] = k, v, n
+            got["done"][b, j] = fin or v == EOS or n >= lim[b]
+            got["src"][b, j] = -1 if got["done"][b, j] else b * K + k
+    return {"scores": scores, **got, "flags": np.zeros(B, np.int32)}
+
+
+def _exact_attend(case, st):
+    S, H, dh, ps = case["B"] * case["K"], case["kv_heads"], case["dh"], case["ps"]
+    G = case["heads"] // H
+    table, lens = st["table"].cpu().numpy(), st["lens"].cpu().numpy()
+
+    def bf16_side(x, up):              # the bfloat16 next to x on one side, or x
+        y = x.to(torch.bfloat16)
+        past = (y.double() < x) if up else (y.double() > x)
+        return torch.where(past, torch.nextafter(y, torch.full_like(y, math.inf if up else -math.inf)), y).double()
+
+    def stored(x):                     # a token's head vectors as the cache holds them
+        if case["cache"] != "int4":
+            return x.double()
+        x = x.double().unflatten(-1, (_groups(dh), -1))
+        least = bf16_side(x.amin(-1, keepdim=True), False)
+        step = bf16_side((x.amax(-1, keepdim=True) - least) / 15, True)
+        return (least + step * torch.round((x - least) / step).clamp(0, 15)).flatten(-2)
+
+    def whole(name, ids, n):           # [n][kv heads][dh] of a sequence
+        t = st[name][0][ids]
+        if case["cache"] == "int4":
+            w = torch.stack([t & 15, t >> 4], -1).flatten(-2).unflatten(-1, (-1, 8))
+            t = torch.stack([w[..., e // 2 + 4 * (e % 2)] for e in range(8)], -1).flatten(-2)
+        t = t.double()
+        if name == "v":
+            t = t.mT
+        if case["cache"] == "int4":
+            f = st[name + "_scale"][0][ids].double()
+            t = (t.unflatten(-1, (_groups(dh), -1)) * f[..., :1] + f[..., 1:]).flatten(-2)
+        return t.transpose(1, 2).flatten(0, 1)[:n].clone()
+
+    out = torch.empty((S, H * G, dh), dtype=torch.float64, device="cuda")
+    if case["append"]:
+        nk, nv = stored(st["new_k"]), stored(st["new_v"])
+    for s in range(S):
+        n = int(lens[s])
+        ids = torch.from_numpy(table[s, :-(-n // ps)].astype(np.int64)).cuda()
+        k, v = whole("k", ids, n), whole("v", ids, n)
+        if case["append"]:
+            k[n - 1], v[n - 1] = nk[s], nv[s]
+        w = torch.softmax((st["q"][s].double().view(H, G, dh) @ k.permute(1, 2, 0).contiguous()) / math.sqrt(dh), -1)
+        out[s] = (w @ v.transpose(0, 1).contiguous()).flatten(0, 1)
+    if not case["append"]:
+        return {"out": out}
+    if case["cache"] == "int4":
+        return {"out": out, "k": nk, "v": nv}
+    return {"out": out, "k": None, "v": None}
