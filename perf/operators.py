@@ -24,8 +24,10 @@ import torch
 
 own = False
 
-if own:
+
+def _pdec():
     from paper_2305_10427_amd import pdec
+    return pdec
 
 
 # --- cases ---------------------------------------------------------------------
@@ -252,8 +254,9 @@ def _cache(st):
     """The cache object that a program keeps beside its tensors."""
     if "handle" not in st:
         c = st["case"]
-        st["handle"] = pdec.PagedCache(c["cache"], c.get("layers", 1), st["k"].shape[1], c["ps"], c["kv_heads"], c["dh"],
-                                       k=st["k"], v=st["v"], k_scale=st.get("k_scale"), v_scale=st.get("v_scale"))
+        st["handle"] = _pdec().PagedCache(c["cache"], c.get("layers", 1), st["k"].shape[1], c["ps"], c["kv_heads"],
+                                          c["dh"], k=st["k"], v=st["v"], k_scale=st.get("k_scale"),
+                                          v_scale=st.get("v_scale"))
     return st["handle"]
 
 
@@ -274,8 +277,8 @@ def run(st):
 def _run_select(st):
     c = st["case"]
     if own:
-        r = pdec.beam_select(st["logits"], st["scores"], st["lens"], st["done"], eos_id=EOS, pad_id=PAD,
-                             alpha=c["alpha"], max_len=st["limit"])
+        r = _pdec().beam_select(st["logits"], st["scores"], st["lens"], st["done"], eos_id=EOS, pad_id=PAD,
+                                 alpha=c["alpha"], max_len=st["limit"])
         return {"scores": r.scores, "parents": r.parents, "tokens": r.tokens, "lens": r.lens, "done": r.done, "src": r.src,
                 "flags": r.flags}
     # keys are compared with each other across rows: 64 bits, or near keys change places
