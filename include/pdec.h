@@ -375,6 +375,165 @@ pd_status pd_decode_traced_static(pd_ctx* ctx, int32_t mode, int32_t block, int3
                                   int32_t* out_k, int32_t* out_flags, void* dev_records, int64_t capacity,
                                   void* stream);
 
+/*
+ * Beam search's operators.  pd_beam_select chooses the surviving hypotheses of
+ * a step; a paged cache (pd_cache) holds the decoder's keys and values so that
+ * hypotheses share the pages of their common prefix; pd_pages_fork makes the
+ * cache follow the survivors; pd_cache_attend appends a token and attends.
+ * They work on caller-owned device buffers of the current device, are enqueued
+ * on the given stream, allocate nothing and can be captured into a graph.  A
+ * workspace (256-byte aligned, at least the bytes its *_bytes call names for
+ * the same sizes; uninitialised) is scratch of one call: calls that may run at
+ * the same time need one each.  Sizes and pointers are checked on the host;
+ * values in device memory (table entries, lengths, parents) are checked by the
+ * kernels, which never read or write outside the buffers described here.
+ */
+
+/* Storage type of a cache in 4 bits (pd_cache only). */
+enum { PD_INT4 = 2 };
+
+/*
+ * One step of beam search: from the logits x[v] of every hypothesis (beam) k of
+ * a sentence, its score s (sum of log-probabilities) and its length n, the
+ * `beam` best continuations of the sentence.
+ *   live beam      done == 0 and s finite: a candidate (k, v) for every word v
+ *                  with x[v] finite, of score s + x[v] - log sum_w exp(x[w]);
+ *   finished beam  done != 0 and s finite: one candidate, itself, with its
+ *                  score and length and the token pad_id; its logits are not read;
+ *   otherwise (s = -inf, as beams 1 .. beam - 1 of a first step): none.
+ * Candidates are ranked by score / length^alpha (length: n + 1, for a finished
+ * beam n; alpha = 0: the plain sum), compared in double; equal keys go to the
+ * lower beam, within a beam to the larger logit and then the lower word.  NaN
+ * and +inf logits are left out like -inf and flagged.
+ *   logits   device, dtype PD_F32 or PD_BF16, [B * beam] rows of vocab values,
+ *            ld elements apart (any alignment of its element)
+ *   scores, lens, done  device [B][beam]; max_len device [B] or NULL: a
+ *            hypothesis that reaches max_len[b] tokens is finished
+ *   out_*    device [B][beam], best first: score, parent (beam of the same
+ *            sentence), token, length, done (token == eos_id, max_len reached,
+ *            or finished before) and src: b * beam + parent, or -1 where done,
+ *            the parents that pd_pages_fork takes.  A place no candidate is
+ *            left for has score -inf, parent -1, token pad_id, length 0, done 1.
+ *            out_scores, out_len, out_done may be scores, lens, done themselves.
+ *   out_flags device [B]: PD_FLAG_NONFINITE if a live beam had a NaN or +inf logit
+ * 1 <= beam <= 64; vocab <= 2^24 (fewer words than beams are allowed).
+ */
+pd_status pd_beam_select_bytes(int32_t dtype, int32_t B, int32_t beam, int32_t vocab, size_t* bytes);
+pd_status pd_beam_select(const void* logits, int32_t dtype, int64_t ld, int32_t B, int32_t beam, int32_t vocab,
+                         const float* scores, const int32_t* lens, const int32_t* done, const int32_t* max_len,
+                         int32_t eos_id, int32_t pad_id, float alpha, float* out_scores, int32_t* out_parent,
+                         int32_t* out_token, int32_t* out_len, int32_t* out_done, int32_t* out_src,
+                         int32_t* out_flags, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A pool of pages that holds keys and values of `layers` layers; one page table
+ * serves them all: page p of layer l is the p-th page of that layer.
+ *   dtype      PD_F32, PD_BF16 or PD_INT4
+ *   page_size  tokens per page: 16, 32, 64 or 128
+ *   head_dim   16, 32, 64 or 128
+ *   k          [layers][pages][kv_heads][page_size][head_dim]
+ *   v          [layers][pages][kv_heads][head_dim][page_size]
+ * (16-byte aligned, caller-owned; pd_cache_bytes names the size of k and of v,
+ * and of each scale array).  PD_INT4 packs the last axis, eight values to a
+ * 32-bit word, value e of a word at bit 4 (e / 2 + 4 (e % 2)), and needs
+ *   k_scale, v_scale  bfloat16 [layers][pages][kv_heads][page_size][groups][2]:
+ *              (step, least) of each group of min(head_dim, 32) dimensions of
+ *              a token's head vector; a code c stands for least + c * step.
+ * A written group has least = its minimum rounded down to bfloat16, step = the
+ * smallest bfloat16 with 15 step >= maximum - least, and the nearest codes
+ * (ties to even): every value within half a step.  A group with a value that
+ * is not finite reads back as NaN.
+ */
+typedef struct {
+  int32_t dtype, layers, pages, page_size, kv_heads, head_dim;
+  void* k;
+  void* v;
+  void* k_scale;
+  void* v_scale;
+} pd_cache;
+
+pd_status pd_cache_bytes(const pd_cache* cache, size_t* kv_bytes, size_t* scale_bytes);
+
+/*
+ * Attention of one token per sequence over a layer of the cache, in float:
+ *   out[s][h] = sum_j p_j v_j,  p = softmax over j < lens[s] of scale q[s][h] . k_j
+ * with the key and value of head h / (heads / kv_heads) in slot j % page_size
+ * of page table[s][j / page_size].
+ *   q, out   device, PD_F32 or PD_BF16 each, rows of heads * head_dim values
+ *            q_ld / out_ld elements apart (a multiple of 8; 16-byte aligned
+ *            bases).  heads is a multiple of kv_heads, at most 16 times it.
+ *   new_k, new_v  NULL, or rows of kv_heads * head_dim values (new_dtype,
+ *            new_ld): the key and value of position lens[s] - 1, written to its
+ *            page in the cache's type before the attention, which reads them
+ *            as the cache holds them.  The page that is written must belong to
+ *            one sequence alone (as pd_pages_fork leaves it).
+ *   table    device int32 [n_seqs][table_ld] page ids, lens device int32
+ *            [n_seqs].  A length counts up to max_len (host) and the table's
+ *            row; keys of a page id outside the pool are left out and nothing
+ *            is written there.  A row with no keys comes out zero.
+ *   group    the n_seqs sequences come in groups of this many (the beams of a
+ *            sentence) which are evaluated together, a page that several of
+ *            them share being read once.  Affects speed only (and rounding).
+ * out must not overlap any other buffer of the call.
+ */
+pd_status pd_cache_attend_bytes(const pd_cache* cache, int32_t heads, int32_t n_seqs, int32_t group, int32_t max_len,
+                                size_t* bytes);
+pd_status pd_cache_attend(const pd_cache* cache, int32_t layer, const void* q, int32_t q_dtype, int64_t q_ld,
+                          int32_t heads, const void* new_k, const void* new_v, int32_t new_dtype, int64_t new_ld,
+                          const int32_t* table, int32_t table_ld, const int32_t* lens, int32_t n_seqs, int32_t group,
+                          int32_t max_len, float scale, void* out, int32_t out_dtype, int64_t out_ld, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * Values that a layer of the cache holds (inspection and export): positions
+ * first[s] .. first[s] + count - 1 of each sequence into out_k, out_v, device
+ * float [n_seqs][count][kv_heads][head_dim]; zero at positions outside
+ * [0, lens[s]) and for pages outside the pool.  first: device int32 [n_seqs].
+ */
+pd_status pd_cache_read(const pd_cache* cache, int32_t layer, const int32_t* table, int32_t table_ld,
+                        const int32_t* lens, int32_t n_seqs, const int32_t* first, int32_t count, float* out_k,
+                        float* out_v, void* stream);
+
+/*
+ * A new page table for the pool, by parents: sequence s of the n_out new ones
+ * takes over the pages of the old sequence parents[s] (-1 or out of range: it
+ * is empty).  A page that no new sequence refers to is free; the table is
+ * taken to hold every reference to the pool.  With grow != 0 every sequence
+ * with a parent also gets the slot of its next token: out_lens = lens + 1, and
+ * the page of that slot belongs to it alone.  On a page border that is a free
+ * page; otherwise the parent's last page, which is kept by the first sequence
+ * that grows into it if every other reference to it grows too, and is copied
+ * (whole, all layers) to a free page for the others.  Free pages are taken
+ * lowest id first, in the order of s.
+ * One call therefore reorders, copies on write, extends, and frees (-1).
+ *   out_table  device int32 [n_out][table_ld] (-1 behind a sequence's pages),
+ *              out_lens [n_out]: must not overlap table and lens
+ *   out_refs   device int32 [pages]: references to each page in out_table
+ *   out_status device int32 [2]: the sequences that could not get their slot
+ *              (too few free pages, or a full table row), and the pages in use.
+ *              If the first is not zero, nothing was copied and every new
+ *              sequence is empty: the old table is still good.
+ * pd_pages_bytes: the workspace, for n_out sequences (n_seqs of pd_pages_compact).
+ */
+pd_status pd_pages_bytes(const pd_cache* cache, int32_t n_seqs, size_t* bytes);
+pd_status pd_pages_fork(const pd_cache* cache, const int32_t* table, int32_t table_ld, const int32_t* lens,
+                        int32_t n_seqs, const int32_t* parents, int32_t n_out, int32_t grow, int32_t* out_table,
+                        int32_t* out_lens, int32_t* out_refs, int32_t* out_status, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/*
+ * Moves the pages in use (those the n_seqs sequences refer to) to the front of
+ * the pool, so that they are pages 0 .. used - 1: the i-th lowest used id of at
+ * least `used` goes to the i-th lowest free id below it, in every layer.
+ *   out_table  device int32 [n_seqs][table_ld]: the table with the new ids
+ *              (may be the table itself)
+ *   out_remap  device int32 [pages]: the new id of each old page, -1 if free
+ *   out_status device int32 [2]: pages moved, pages in use
+ */
+pd_status pd_pages_compact(const pd_cache* cache, const int32_t* table, int32_t table_ld, const int32_t* lens,
+                           int32_t n_seqs, int32_t* out_table, int32_t* out_remap, int32_t* out_status,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char* pd_last_error(void);
 

@@ -6,9 +6,10 @@ library is missing or fails, calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -50,8 +51,20 @@ EXPORTS = ("pd_weight_count", "pd_weight_shape", "pd_model_create", "pd_model_de
            "pd_ctx_workspace_bytes", "pd_ctx_create", "pd_ctx_destroy", "pd_encode", "pd_decode", "pd_decode_init",
            "pd_debug_logits", "pd_ctx_set_timing", "pd_ctx_vocab_timing", "pd_ctx_rows_processed",
            "pd_trace_scratch_bytes", "pd_ctx_set_trace", "pd_ctx_trace_count", "pd_ctx_product_timing",
-           "pd_ctx_iteration_kernels", "pd_decode_traced_static", "pd_last_error")
+           "pd_ctx_iteration_kernels", "pd_decode_traced_static", "pd_beam_select_bytes", "pd_beam_select",
+           "pd_cache_bytes", "pd_cache_attend_bytes", "pd_cache_attend", "pd_cache_read", "pd_pages_bytes",
+           "pd_pages_fork", "pd_pages_compact", "pd_last_error")
 TRACE_STATIC_BYTES = 8 << 20      # PD_TRACE_STATIC_BYTES
+
+CACHE_TYPES = {"f32": 0, "bf16": 1, "int4": 2}      # PD_F32, PD_BF16, PD_INT4
+
+
+class pd_cache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("layers", ctypes.c_int32), ("pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p)]
+
 
 _lib = None
 
@@ -105,6 +118,27 @@ def load_library(path: str = LIB_PATH):
     L.pd_ctx_iteration_kernels.restype = I32
     L.pd_decode_traced_static.argtypes = [VP, I32, I32, I32, I32, P(I32), VP, I32, VP, VP, VP, VP, I64, VP]
     L.pd_decode_traced_static.restype = I32
+    F32, PC = ctypes.c_float, P(pd_cache)
+    L.pd_beam_select_bytes.argtypes = [I32, I32, I32, I32, P(SZ)]
+    L.pd_beam_select_bytes.restype = I32
+    L.pd_beam_select.argtypes = [VP, I32, I64, I32, I32, I32, VP, VP, VP, VP, I32, I32, F32, VP, VP, VP, VP, VP, VP,
+                                 VP, VP, SZ, VP]
+    L.pd_beam_select.restype = I32
+    L.pd_cache_bytes.argtypes = [PC, P(SZ), P(SZ)]
+    L.pd_cache_bytes.restype = I32
+    L.pd_cache_attend_bytes.argtypes = [PC, I32, I32, I32, I32, P(SZ)]
+    L.pd_cache_attend_bytes.restype = I32
+    L.pd_cache_attend.argtypes = [PC, I32, VP, I32, I64, I32, VP, VP, I32, I64, VP, I32, VP, I32, I32, I32, F32, VP,
+                                  I32, I64, VP, SZ, VP]
+    L.pd_cache_attend.restype = I32
+    L.pd_cache_read.argtypes = [PC, I32, VP, I32, VP, I32, VP, I32, VP, VP, VP]
+    L.pd_cache_read.restype = I32
+    L.pd_pages_bytes.argtypes = [PC, I32, P(SZ)]
+    L.pd_pages_bytes.restype = I32
+    L.pd_pages_fork.argtypes = [PC, VP, I32, VP, I32, VP, I32, I32, VP, VP, VP, VP, VP, SZ, VP]
+    L.pd_pages_fork.restype = I32
+    L.pd_pages_compact.argtypes = [PC, VP, I32, VP, I32, VP, VP, VP, VP, SZ, VP]
+    L.pd_pages_compact.restype = I32
     L.pd_last_error.argtypes = []
     L.pd_last_error.restype = ctypes.c_char_p
     _lib = L
@@ -339,3 +373,237 @@ class Context:
         if getattr(self, "handle", None) and _lib is not None:
             _lib.pd_ctx_destroy(self.handle)
             self.handle = None
+
+
+# --- beam search's operators ---------------------------------------------------
+
+
+class BeamStep(NamedTuple):
+    """Survivors of a step, [B, beam] each, best first (flags [B]): see pd_beam_select."""
+    scores: object
+    parents: object
+    tokens: object
+    lens: object
+    done: object
+    src: object
+    flags: object
+
+
+class PageFork(NamedTuple):
+    """New table, lengths, references per page, and (sequences without a slot, pages in use)."""
+    table: object
+    lens: object
+    refs: object
+    status: object
+
+
+class PageMoves(NamedTuple):
+    """Table with the new ids, new id of each page (-1: free), and (pages moved, pages in use)."""
+    table: object
+    remap: object
+    status: object
+
+
+def _scope(dev, stream):
+    """Makes `stream` (default: the current stream of `dev`) current, so that outputs and scratch belong to it."""
+    import torch
+    if stream is not None:
+        if stream.device != dev:
+            raise PdError(1, f"the stream is on {stream.device}, the tensors are on {dev}")
+        return torch.cuda.stream(stream)
+    if dev.type == "cuda" and dev.index != torch.cuda.current_device():
+        return torch.cuda.device(dev)
+    return contextlib.nullcontext()
+
+
+def _tensor(name, t, dtypes, shape, dev, contiguous=True):
+    """Refuses anything but a tensor of one of the dtypes, of the shape (None: any size) on the device."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+        raise PdError(1, f"{name} must be a tensor of {' or '.join(str(d) for d in dtypes)}")
+    if t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
+        raise PdError(2, f"{name} has shape {tuple(t.shape)}, expected {tuple('any' if w is None else w for w in shape)}")
+    if t.device != dev or dev.type != "cuda":
+        raise PdError(1, f"{name} is on {t.device}: every tensor of a call belongs on one GPU")
+    if contiguous and not t.is_contiguous():
+        raise PdError(1, f"{name} must be contiguous")
+    return t
+
+
+def _rows(name, t):
+    """Elements from one row of a 3-D tensor to the next: the last two dimensions packed, rows of any distance."""
+    n = t.shape[2]
+    if (t.shape[2] > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != n):
+        raise PdError(1, f"the rows of {name} must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * n
+
+
+def beam_select(logits, scores, lens, done, *, eos_id: int = C.EOS_ID, pad_id: int = C.PAD_ID, alpha: float = 1.0,
+                max_len=None, stream=None) -> BeamStep:
+    """One step of beam search (pd_beam_select): logits [B, beam, V] float32 or bfloat16 (rows of any distance,
+    the beams of a sentence evenly spaced), scores float32, lens and done int32 [B, beam], max_len int32 [B] or None."""
+    import torch
+    L = load_library()
+    dev = scores.device
+    f32, i32 = (torch.float32,), (torch.int32,)
+    _tensor("logits", logits, (torch.float32, torch.bfloat16), (None, None, None), dev, contiguous=False)
+    B, K, V = logits.shape
+    ld = logits.stride(1) if K > 1 else logits.stride(0) if B > 1 else V
+    if (V > 1 and logits.stride(2) != 1) or (B > 1 and logits.stride(0) != K * ld):
+        raise PdError(1, "the rows of logits must be contiguous and evenly spaced")
+    _tensor("scores", scores, f32, (B, K), dev)
+    _tensor("lens", lens, i32, (B, K), dev)
+    _tensor("done", done, i32, (B, K), dev)
+    if max_len is not None:
+        _tensor("max_len", max_len, i32, (B,), dev)
+    dt = 1 if logits.dtype == torch.bfloat16 else 0
+    n = ctypes.c_size_t()
+    _check(L.pd_beam_select_bytes(dt, B, K, V, ctypes.byref(n)))
+    with _scope(dev, stream):
+        out = torch.empty_like(scores)
+        ints = torch.empty((5, B, K), dtype=torch.int32, device=dev)
+        flags = torch.empty(B, dtype=torch.int32, device=dev)
+        ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
+        at, step = ints.data_ptr(), 4 * B * K
+        _check(L.pd_beam_select(logits.data_ptr(), dt, ld, B, K, V, scores.data_ptr(), lens.data_ptr(),
+                                done.data_ptr(), max_len.data_ptr() if max_len is not None else None, eos_id, pad_id,
+                                alpha, out.data_ptr(), at, at + step, at + 2 * step, at + 3 * step, at + 4 * step,
+                                flags.data_ptr(), ws.data_ptr(), n.value, _stream_handle(None)))
+    return BeamStep(out, *ints.unbind(0), flags)
+
+
+class PagedCache:
+    """A pool of pages of keys and values (pd_cache): dtype "f32", "bf16" or "int4", layouts as pdec.h states.
+
+    The tensors are allocated here (zeroed) unless given.  Page tables are int32 [sequences, pages], lengths int32."""
+
+    def __init__(self, dtype: str, layers: int, pages: int, page_size: int, kv_heads: int, head_dim: int, *, k=None,
+                 v=None, k_scale=None, v_scale=None, device="cuda"):
+        import torch
+        if dtype not in CACHE_TYPES:
+            raise PdError(1, f"unknown cache dtype {dtype!r}")
+        c = pd_cache(CACHE_TYPES[dtype], layers, pages, page_size, kv_heads, head_dim)
+        kv, sc = ctypes.c_size_t(), ctypes.c_size_t()
+        _check(load_library().pd_cache_bytes(ctypes.byref(c), ctypes.byref(kv), ctypes.byref(sc)))
+        t = {"f32": torch.float32, "bf16": torch.bfloat16, "int4": torch.uint8}[dtype]
+        pack = 2 if dtype == "int4" else 1
+        head = (layers, pages, kv_heads)
+        shapes = {"k": (t, head + (page_size, head_dim // pack)), "v": (t, head + (head_dim, page_size // pack))}
+        if dtype == "int4":
+            shapes["k_scale"] = shapes["v_scale"] = (torch.bfloat16, head + (page_size, max(1, head_dim // 32), 2))
+        given = {"k": k, "v": v, "k_scale": k_scale, "v_scale": v_scale}
+        dev = k.device if k is not None else torch.empty(0, device=device).device
+        for name, x in given.items():
+            if name not in shapes:
+                if x is not None:
+                    raise PdError(1, f"{name} is for a cache in 4 bits")
+                setattr(self, name, None)
+                continue
+            dt, shape = shapes[name]
+            if x is None:
+                x = torch.zeros(shape, dtype=dt, device=dev)
+            setattr(self, name, _tensor(name, x, (dt,), shape, dev))
+            setattr(c, name, x.data_ptr())
+        self.dtype, self.layers, self.pages, self.page_size = dtype, layers, pages, page_size
+        self.kv_heads, self.head_dim, self.device = kv_heads, head_dim, dev
+        self._c = c
+        self._p = ctypes.byref(c)
+        self._need = {}                      # workspace bytes by sizes
+
+    def _table(self, table, lens):
+        import torch
+        _tensor("table", table, (torch.int32,), (None, None), self.device)
+        _tensor("lens", lens, (torch.int32,), (table.shape[0],), self.device)
+        return table.shape
+
+    def _bytes(self, fn, *sizes):
+        key = (fn,) + sizes
+        if key not in self._need:
+            n = ctypes.c_size_t()
+            _check(getattr(load_library(), fn)(self._p, *sizes, ctypes.byref(n)))
+            self._need[key] = n.value
+        return self._need[key]
+
+    def attend(self, q, table, lens, *, layer: int = 0, group: int = 1, max_len: Optional[int] = None, new_k=None,
+               new_v=None, out_dtype=None, scale: Optional[float] = None, stream=None):
+        """out [S, heads, head_dim] of q [S, heads, head_dim] over each sequence's keys (pd_cache_attend); new_k and
+        new_v [S, kv_heads, head_dim] are appended at position lens - 1 first.  max_len: a bound on the lengths
+        (default: what the table can name); out_dtype: float32 or bfloat16 (default: q's)."""
+        import torch
+        L = load_library()
+        S, ld = self._table(table, lens)
+        types = (torch.float32, torch.bfloat16)
+        _tensor("q", q, types, (S, None, self.head_dim), self.device, contiguous=False)
+        H = q.shape[1]
+        odt = q.dtype if out_dtype is None else out_dtype
+        if odt not in types:
+            raise PdError(1, "out_dtype must be torch.float32 or torch.bfloat16")
+        if (new_k is None) != (new_v is None):
+            raise PdError(1, "new_k and new_v go together")
+        kp = vp = None
+        ndt = nld = 0
+        if new_k is not None:
+            for name, x in (("new_k", new_k), ("new_v", new_v)):
+                _tensor(name, x, types, (S, self.kv_heads, self.head_dim), self.device, contiguous=False)
+            nld = _rows("new_k", new_k)
+            if new_v.dtype != new_k.dtype or _rows("new_v", new_v) != nld:
+                raise PdError(1, "new_k and new_v must have the same type and row distance")
+            kp, vp, ndt = new_k.data_ptr(), new_v.data_ptr(), int(new_k.dtype == torch.bfloat16)
+        top = ld * self.page_size if max_len is None else max_len
+        n = self._bytes("pd_cache_attend_bytes", H, S, group, top)
+        with _scope(self.device, stream):
+            out = torch.empty((S, H, self.head_dim), dtype=odt, device=self.device)
+            ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+            _check(L.pd_cache_attend(self._p, layer, q.data_ptr(), int(q.dtype == torch.bfloat16), _rows("q", q), H, kp,
+                                     vp, ndt, nld, table.data_ptr(), ld, lens.data_ptr(), S, group, top,
+                                     self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
+                                     int(odt == torch.bfloat16), H * self.head_dim, ws.data_ptr() if n else None, n,
+                                     _stream_handle(None)))
+        return out
+
+    def read(self, table, lens, first, *, layer: int = 0, count: int = 1, stream=None):
+        """Values held at positions first .. first + count - 1 of each sequence, float32
+        ([S, count, kv_heads, head_dim] of keys, of values); zero outside the sequence."""
+        import torch
+        S, ld = self._table(table, lens)
+        _tensor("first", first, (torch.int32,), (S,), self.device)
+        with _scope(self.device, stream):
+            k, v = (torch.empty((S, max(count, 1), self.kv_heads, self.head_dim), dtype=torch.float32, device=self.device)
+                    for _ in range(2))
+            _check(load_library().pd_cache_read(self._p, layer, table.data_ptr(), ld, lens.data_ptr(), S,
+                                                first.data_ptr(), count, k.data_ptr(), v.data_ptr(),
+                                                _stream_handle(None)))
+        return k, v
+
+    def fork(self, table, lens, parents, *, grow: bool = True, stream=None) -> PageFork:
+        """The table of the sequences whose parents are given (-1: empty), with a slot for the next token if grow
+        (pd_pages_fork)."""
+        import torch
+        S, ld = self._table(table, lens)
+        _tensor("parents", parents, (torch.int32,), (None,), self.device)
+        n_out = parents.shape[0]
+        n = self._bytes("pd_pages_bytes", n_out)
+        with _scope(self.device, stream):
+            new = torch.empty((n_out, ld), dtype=torch.int32, device=self.device)
+            rest = torch.empty(n_out + self.pages + 2, dtype=torch.int32, device=self.device)
+            out_lens, refs, status = rest.split((n_out, self.pages, 2))
+            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+            _check(load_library().pd_pages_fork(self._p, table.data_ptr(), ld, lens.data_ptr(), S, parents.data_ptr(),
+                                                n_out, int(grow), new.data_ptr(), out_lens.data_ptr(), refs.data_ptr(),
+                                                status.data_ptr(), ws.data_ptr(), n, _stream_handle(None)))
+        return PageFork(new, out_lens, refs, status)
+
+    def compact(self, table, lens, *, stream=None) -> PageMoves:
+        """Moves the pages in use to the front of the pool (pd_pages_compact)."""
+        import torch
+        S, ld = self._table(table, lens)
+        n = self._bytes("pd_pages_bytes", S)
+        with _scope(self.device, stream):
+            new = torch.empty((S, ld), dtype=torch.int32, device=self.device)
+            rest = torch.empty(self.pages + 2, dtype=torch.int32, device=self.device)
+            remap, status = rest.split((self.pages, 2))
+            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+            _check(load_library().pd_pages_compact(self._p, table.data_ptr(), ld, lens.data_ptr(), S, new.data_ptr(),
+                                                   remap.data_ptr(), status.data_ptr(), ws.data_ptr(), n,
+                                                   _stream_handle(None)))
+        return PageMoves(new, remap, status)

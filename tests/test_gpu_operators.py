@@ -1,0 +1,679 @@
+"""The beam-search operators on the GPU against plain 64-bit implementations (tests/operators_ref.py).
+
+Attention tolerance (derived, u = 2^-24).  A score is scale times a sum of dh
+products in float of exact cache values: off by at most
+(dh + 8) 2u scale sum_d |q_d| a_d, where a is |k|, or for a cache in 4 bits the
+magnitudes the linear form adds up, (256 + code) step + |least| (codes enter the
+products with an offset of 128).  A weight is then off by twice the largest such
+error, plus 2^-21 (exponentials), plus (n + 64) u (the sum of n weights), and the
+output by that relative to sum_j p_j a_j, plus 2^-17 (weights enter the product
+in two bfloat16 parts, 2^-18), plus (n + 64) u (its own sum).  Storing rounds by
+half a step, finfo(t).eps / 2 of the value.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2305_10427_amd import pdec
+from tests import operators_ref as R
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def gpu(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a))
+    return (t if dtype is None else t.to(dtype)).cuda()
+
+
+def i32(a):
+    return gpu(np.asarray(a), torch.int32)
+
+
+def host(t):
+    return t.double().cpu().numpy() if t.is_floating_point() else t.cpu().numpy()
+
+
+# --- a pool with known values ------------------------------------------------------
+
+
+class Pool:
+    """A PagedCache of random values; k, v [layers][pages][kv][ps][dh] hold them in 64 bits, ak, av the magnitudes of
+    the tolerance."""
+
+    def __init__(self, g, dtype, layers, pages, ps, kv, dh):
+        self.dtype, self.ps, self.kv, self.dh, self.pages = dtype, ps, kv, dh, pages
+        shape = (layers, pages, kv, ps, dh)
+        if dtype == "int4":
+            G = max(1, dh // 32)
+            self.cache = pdec.PagedCache(dtype, layers, pages, ps, kv, dh)
+            for n in "kv":
+                code = g.integers(0, 16, shape)
+                step = 0.1 + 0.3 * g.random((layers, pages, kv, ps, G))
+                par = torch.from_numpy(np.stack([step, -7.5 * step + 0.5 * g.normal(size=step.shape)], -1)).to(torch.bfloat16)
+                getattr(self.cache, n + "_scale").copy_(par)
+                step, least = par.double().numpy()[..., 0], par.double().numpy()[..., 1]
+                rep = lambda x: np.repeat(x, dh // G, -1)  # noqa: E731
+                setattr(self, n, code * rep(step) + rep(least))
+                setattr(self, "a" + n, (256 + code) * rep(step) + np.abs(rep(least)))
+                getattr(self.cache, n).copy_(torch.from_numpy(R.pack(code if n == "k" else code.swapaxes(-1, -2))))
+        else:
+            t = {n: torch.from_numpy(g.normal(size=shape)).to(TYPES[dtype]) for n in "kv"}
+            self.cache = pdec.PagedCache(dtype, layers, pages, ps, kv, dh, k=t["k"].cuda(),
+                                         v=t["v"].transpose(-1, -2).contiguous().cuda())
+            for n in "kv":
+                setattr(self, n, t[n].double().numpy())
+                setattr(self, "a" + n, np.abs(getattr(self, n)))
+
+    def tensors(self):
+        return {n: getattr(self.cache, n) for n in ("k", "v", "k_scale", "v_scale") if getattr(self.cache, n) is not None}
+
+    def take(self, name, layer, row, n):
+        """[n][kv][dh] of a sequence whose pages are `row`; keys of pages outside the pool are left out."""
+        a = getattr(self, name)[layer]
+        out = [a[row[j // self.ps], :, j % self.ps] for j in range(n) if 0 <= row[j // self.ps] < self.pages]
+        return np.array(out).reshape(len(out), self.kv, self.dh)
+
+    def sync_from_gpu(self):
+        """Reads the pool's values back (float64), layouts undone on the host."""
+        got = {}
+        for n in "kv":
+            t = getattr(self.cache, n).cpu()
+            if self.dtype == "int4":
+                code = R.unpack(t.numpy())
+                code = code.swapaxes(-1, -2) if n == "v" else code
+                par = getattr(self.cache, n + "_scale").double().cpu().numpy()
+                got[n] = R.dequantise(code, par[..., 0], par[..., 1])
+            else:
+                got[n] = (t.transpose(-1, -2) if n == "v" else t).double().numpy()
+        return got
+
+
+def tree_tables(g, lens, group, ps, pages, share, ld):
+    """Tables of sequences in groups: each takes a random part of an earlier one's full pages, the rest are its own."""
+    ids = iter(g.permutation(pages))
+    table = np.full((len(lens), ld), -1, np.int64)
+    for s, n in enumerate(lens):
+        need, common = -(-n // ps), 0
+        if s % group and share:
+            o = s - 1 - int(g.integers(0, s % group))
+            common = min(int(g.integers(0, n // ps + 1)), lens[o] // ps)
+            table[s, :common] = table[o, :common]
+        for j in range(common, need):
+            table[s, j] = next(ids)
+    return table
+
+
+def bound(pool, layer, q, ref, w, row, n, scale, out_dtype):
+    ak, av = pool.take("ak", layer, row, n), pool.take("av", layer, row, n)
+    H, kv = q.shape[0], pool.kv
+    m = len(ak)
+    tol = np.zeros_like(ref)
+    for h in range(H if m else 0):
+        ds = (pool.dh + 8) * 2 * U * abs(scale) * (ak[:, h // (H // kv)] @ np.abs(q[h]))
+        rel = 2 * ds.max() + 2.0 ** -21 + (m + 64) * U
+        tol[h] = (2 * rel + 2.0 ** -17 + (m + 64) * U) * (w[h] @ av[:, h // (H // kv)])
+    return tol + (np.abs(ref) + tol) * torch.finfo(out_dtype).eps / 2 + 1e-30
+
+
+def check(pool, out, q, table, lens, *, layer=0, scale=None, cut=None, skip=()):
+    scale = pool.dh ** -0.5 if scale is None else scale
+    got, qh = host(out), host(q)
+    ld = table.shape[1]
+    for s in range(len(lens)):
+        if s in skip:
+            continue
+        n = min(max(int(lens[s]), 0), ld * pool.ps, cut or 1 << 40)
+        k, v = pool.take("k", layer, table[s], n), pool.take("v", layer, table[s], n)
+        ref, w = R.attend(qh[s], k, v, scale)
+        err = np.abs(got[s] - ref)
+        tol = bound(pool, layer, qh[s], ref, w, table[s], n, scale, out.dtype)
+        assert (err <= tol).all(), (s, n, float((err / tol).max()))
+
+
+ATTEND = [
+    # cache, heads, kv, dh, ps, group, lengths, share, q, out
+    ("f32", 4, 4, 16, 16, 4, [16, 16, 16, 16, 1, 1, 1, 1], True, "f32", "f32"),
+    ("f32", 8, 8, 64, 32, 5, [0, 1, 31, 32, 33] + [70] * 5, True, "f32", "f32"),
+    ("f32", 8, 2, 128, 64, 2, [65, 64, 130, 127], True, "bf16", "bf16"),
+    ("f32", 16, 1, 32, 16, 3, [15, 17, 16], False, "f32", "f32"),
+    ("bf16", 8, 8, 64, 16, 5, [5, 16, 17, 0, 47] + [138] * 5 + [1, 2, 3, 4, 300], True, "f32", "bf16"),
+    ("bf16", 16, 16, 64, 128, 1, [129, 128, 1, 500], False, "f32", "f32"),
+    ("bf16", 6, 2, 128, 32, 4, [63, 64, 65, 31], True, "f32", "f32"),
+    ("bf16", 4, 4, 16, 64, 16, [77] * 16, True, "bf16", "bf16"),
+    ("bf16", 10, 5, 32, 16, 1, [1], False, "f32", "f32"),
+    ("int4", 16, 16, 64, 16, 5, [30, 1, 16, 0, 33] + [256] * 5, True, "f32", "f32"),
+    ("int4", 8, 4, 128, 32, 4, [129, 130, 131, 132], True, "f32", "f32"),
+    ("int4", 4, 4, 16, 16, 2, [9, 41], True, "f32", "bf16"),
+    ("int4", 12, 3, 32, 128, 3, [127, 128, 129], True, "bf16", "f32"),
+    ("bf16", 2, 2, 32, 16, 24, [33] * 24, True, "f32", "f32"),          # more rows than one tile of the matrix cores
+    ("int4", 32, 2, 64, 16, 3, [50, 64, 65], True, "f32", "f32"),       # sixteen query heads share a key head
+    ("f32", 9, 3, 16, 16, 11, [40] * 22, True, "f32", "f32"),
+    # a long axis with few rows
+    ("bf16", 4, 4, 64, 16, 1, [5003], False, "f32", "f32"),
+    ("int4", 8, 2, 128, 64, 2, [9001, 8999], True, "f32", "f32"),
+    ("f32", 2, 2, 32, 32, 3, [3001, 2047, 1], True, "f32", "f32"),
+]
+
+
+@pytest.mark.parametrize("case", ATTEND, ids=lambda c: f"{c[0]}-h{c[1]}:{c[2]}x{c[3]}-p{c[4]}-g{c[5]}-{max(c[6])}")
+def test_attention_against_64_bits(case):
+    cache, H, kv, dh, ps, group, lens, share, qt, ot = case
+    say("attend", case)
+    g = np.random.default_rng(len(lens) + dh + H)
+    ld = -(-max(max(lens), 1) // ps) + 1
+    pages = sum(-(-n // ps) for n in lens) + 3
+    pool = Pool(g, cache, 2, pages, ps, kv, dh)
+    table = tree_tables(g, lens, group, ps, pages, share, ld)
+    q = gpu(2 * g.normal(size=(len(lens), H, dh)), TYPES[qt])
+    out = pool.cache.attend(q, i32(table), i32(lens), layer=1, group=group, out_dtype=TYPES[ot])
+    check(pool, out, q, table, lens, layer=1)
+    one = pool.cache.attend(q, i32(table), i32(lens), layer=1, out_dtype=TYPES[ot], scale=0.3, max_len=max(max(lens), 1))
+    check(pool, one, q, table, lens, layer=1, scale=0.3)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "int4"])
+def test_attention_reads_only_a_sequences_own_keys(cache):
+    """NaN in every slot behind a sequence's end and every page that is not its own; one beam's own page holds NaN too."""
+    g = np.random.default_rng(5)
+    ps, kv, dh, lens, group = 16, 2, 32, [37, 37, 45, 37, 20, 16, 33, 1], 4
+    pool = Pool(g, cache, 1, 40, ps, kv, dh)
+    table = tree_tables(g, lens, group, ps, 40, True, 4)
+    q = gpu(g.normal(size=(len(lens), 4, dh)), torch.float32)
+    used = np.zeros((40, ps), bool)
+    for s, n in enumerate(lens):
+        for j in range(n):
+            used[table[s, j // ps], j % ps] = True
+    sick = int(table[2, 2])                                   # sequence 2's last page
+    assert (table == sick).sum() == 1
+    used[sick] = False
+    bad = torch.from_numpy(~used)
+    c = pool.cache
+    if cache == "int4":
+        for t in (c.k_scale, c.v_scale):
+            t[0].masked_fill_(bad[:, None, :, None, None].cuda(), math.nan)
+    else:
+        c.k[0].masked_fill_(bad[:, None, :, None].cuda(), math.nan)
+        c.v[0].masked_fill_(bad[:, None, None, :].cuda(), math.inf)
+    for group in (group, 1):
+        out = c.attend(q, i32(table), i32(lens), group=group)
+        assert torch.isnan(out[2]).all()
+        check(pool, out, q, table, lens, skip=(2,))
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "int4"])
+def test_attention_bounds_lengths_and_pages(cache):
+    g = np.random.default_rng(6)
+    ps, kv, dh = 16, 2, 16
+    pool = Pool(g, cache, 1, 12, ps, kv, dh)
+    table = g.integers(0, 12, (8, 3))
+    table[1, 1], table[2, 0], table[3] = -1, 12, [2 ** 31 - 1, -2 ** 31, -7]
+    table[5] = table[4]
+    lens = [48, 48, 40, 30, -5, 100000, 2 ** 31 - 1, -2 ** 31]
+    q = gpu(g.normal(size=(8, 2, dh)), torch.float32)
+    for group in (1, 2, 4):
+        out = pool.cache.attend(q, i32(table), i32(lens), group=group)
+        check(pool, out, q, table, lens)
+        assert not out[3].any() and not out[4].any() and not out[7].any()
+        check(pool, pool.cache.attend(q, i32(table), i32(lens), group=group, max_len=21), q, table, lens, cut=21)
+
+
+@pytest.mark.parametrize("new", ["f32", "bf16"])
+@pytest.mark.parametrize("cache,dh,ps", [("f32", 16, 16), ("bf16", 64, 32), ("int4", 16, 16), ("int4", 64, 64),
+                                         ("int4", 128, 16)])
+def test_append_writes_one_slot_and_attends_to_it(cache, dh, ps, new):
+    g = np.random.default_rng(dh + ps)
+    kv, H = 3, 6
+    lens = [1, ps, ps + 1, 2 * ps - 1, 0, 2 * ps + 3, 2 * ps + 3, 7, 9, 40]
+    S = len(lens)
+    pool = Pool(g, cache, 2, 40, ps, kv, dh)
+    table = tree_tables(g, lens, 1, ps, 40, False, 4)
+    table[6, :2] = table[5, :2]                                # full pages are shared, the written page is not
+    table[8, 0] = 40                                           # no such page: nothing is written
+    # rows of a fused product: queries, keys and values side by side
+    fused = gpu(g.normal(size=(S, 1, (H + 2 * kv) * dh)) * 2 + 0.7, TYPES[new])
+    cut = lambda a, n: fused[:, 0, a * dh:(a + n) * dh].unflatten(1, (n, dh))  # noqa: E731
+    q, nk, nv = cut(0, H), cut(H, kv), cut(H + kv, kv)
+    before = {n: t.clone() for n, t in pool.tensors().items()}
+    out = pool.cache.attend(q, i32(table), i32(lens), layer=1, group=2, new_k=nk, new_v=nv, out_dtype=torch.float32)
+    # what the slots have to hold, and the pool as it was everywhere else
+    want = {n: getattr(pool, n).copy() for n in "kv"}
+    for n, x in (("k", host(nk)), ("v", host(nv))):
+        if cache == "int4":
+            code, step, least = R.quantise(x)
+            val, mag = R.dequantise(code, step, least), (256 + code) * np.repeat(step, dh // step.shape[-1], -1) + np.abs(
+                np.repeat(least, dh // step.shape[-1], -1))
+        else:
+            val = torch.from_numpy(x).to(TYPES[cache]).double().numpy()
+            mag = np.abs(val)
+        for s, m in enumerate(lens):
+            if m and s != 8:
+                want[n][1, table[s, (m - 1) // ps], :, (m - 1) % ps] = val[s]
+                getattr(pool, "a" + n)[1, table[s, (m - 1) // ps], :, (m - 1) % ps] = mag[s]
+    got = pool.sync_from_gpu()
+    for n in "kv":
+        np.testing.assert_array_equal(got[n], want[n])
+        setattr(pool, n, want[n])
+    for n, t in before.items():
+        assert torch.equal(t[0].view(torch.uint8), pool.tensors()[n][0].view(torch.uint8))      # layer 0
+    check(pool, out, q, table, lens, layer=1)
+    k, v = pool.cache.read(i32(table), i32(lens), i32(lens) - 1, layer=1)
+    for s, m in enumerate(lens):
+        for n, t in (("k", k), ("v", v)):
+            ref = pool.take(n, 1, table[s], m)[-1] if m and s != 8 else np.zeros((kv, dh))
+            np.testing.assert_array_equal(host(t)[s, 0], ref.astype(np.float32) if cache == "int4" else ref)
+
+
+def test_append_of_values_that_are_not_finite_and_of_constants():
+    pool = Pool(np.random.default_rng(1), "int4", 1, 4, 16, 2, 64)
+    x = torch.zeros(3, 2, 64, device="cuda")
+    x[0, 0, 5], x[0, 1, 40], x[1, 0, 63] = math.inf, math.nan, -math.inf
+    x[1, 1], x[2, 0], x[2, 1] = 0.3, 3e38, torch.linspace(-3e38, 3e38, 64, dtype=torch.float64)
+    t, n = i32([[0], [1], [2]]), i32([3, 1, 16])
+    pool.cache.attend(torch.zeros(3, 2, 64, device="cuda"), t, n, new_k=x, new_v=x)
+    for got in pool.cache.read(t, n, n - 1):
+        got = got[:, 0].reshape(3, 2, 2, 32)
+        nan = torch.isnan(got).all(-1).tolist()
+        assert nan == [[[True, False], [False, True]], [[False, True], [False, False]], [[False, False], [False, False]]]
+        assert torch.isnan(got).any(-1).tolist() == nan
+        ref = host(x).reshape(3, 2, 2, 32)
+        for s, h in ((1, 1), (2, 0), (2, 1)):
+            code, step, least = R.quantise(ref[s, h])
+            # 0.3 and 3e38 are no bfloat16 values: within half a step of least + code step, which rounds to float
+            assert (np.abs(host(got)[s, h] - ref[s, h]) <= step / 2 * (1 + 1e-6) + np.abs(ref[s, h]) * U).all()
+
+
+def test_read_ranges():
+    g = np.random.default_rng(8)
+    for cache in ("f32", "bf16", "int4"):
+        pool = Pool(g, cache, 2, 9, 16, 2, 32)
+        table, lens, first = np.array([[3, 1, -1], [0, 9, 2]]), [20, 40], [-2, 14]
+        k, v = pool.cache.read(i32(table), i32(lens), i32(first), layer=1, count=30)
+        for name, t in (("k", k), ("v", v)):
+            ref = np.zeros((2, 30, 2, 32))
+            for s in range(2):
+                for c in range(30):
+                    j = first[s] + c
+                    if 0 <= j < lens[s] and 0 <= table[s, j // 16] < 9:
+                        ref[s, c] = getattr(pool, name)[1, table[s, j // 16], :, j % 16]
+            np.testing.assert_array_equal(host(t), ref.astype(np.float32))
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "int4"])
+def test_offsets_beyond_32_bits(cache):
+    """Pools whose last pages start past 2^32 bytes and 2^31 values."""
+    kv, ps, dh = 16, 128, 128
+    pages = {"f32": 8200, "bf16": 8300, "int4": 33000}[cache]
+    es = {"f32": 4.0, "bf16": 2.0, "int4": 0.5}[cache]
+    assert (pages - 4) * kv * ps * dh * es > 2 ** 32
+    head = (1, pages, kv)
+    t = {"f32": torch.float32, "bf16": torch.bfloat16, "int4": torch.uint8}[cache]
+    pack = 2 if cache == "int4" else 1
+    mk = lambda *s, dt=t: torch.empty(head + s, dtype=dt, device="cuda")  # noqa: E731
+    more = {n: mk(ps, 4, 2, dt=torch.bfloat16) for n in ("k_scale", "v_scale")} if cache == "int4" else {}
+    big = pdec.PagedCache(cache, 1, pages, ps, kv, dh, k=mk(ps, dh // pack), v=mk(dh, ps // pack), **more)
+    g = np.random.default_rng(2)
+    pool = Pool(g, cache, 1, 4, ps, kv, dh)                   # its four pages become the last of the large pool
+    table, lens = np.array([[2, 0], [3, 1]]), [200, 129]
+    for n, x in pool.tensors().items():
+        getattr(big, n)[0, pages - 4:] = x[0]
+    new = gpu(g.normal(size=(2, kv, dh)), torch.float32)
+    q = gpu(g.normal(size=(2, kv, dh)), torch.float32)
+    a = big.attend(q, i32(table + pages - 4), i32(lens), new_k=new, new_v=new)
+    b = pool.cache.attend(q, i32(table), i32(lens), new_k=new, new_v=new)
+    assert torch.equal(a, b)
+    for n, x in pool.tensors().items():
+        assert torch.equal(getattr(big, n)[0, pages - 4:].view(torch.uint8), x[0].view(torch.uint8))
+    # a fork copies between the far ends of the pool; compaction brings the last pages to the front
+    f = big.fork(i32(table + pages - 4), i32(lens), i32([0, 0, 1]))
+    r = R.fork(table + pages - 4, lens, [0, 0, 1], pages, ps, True)
+    assert host(f.table).tolist() == r[0].tolist() and r[4] == [(pages - 4, 0)]
+    for n, x in pool.tensors().items():
+        assert torch.equal(getattr(big, n)[0, 0].view(torch.uint8), x[0, 0].view(torch.uint8))
+    m = big.compact(i32(table + pages - 4), i32(lens))
+    assert m.status.tolist() == [4, 4] and m.table.tolist() == [[2, 0], [3, 1]]
+    for n, x in pool.tensors().items():
+        assert torch.equal(getattr(big, n)[0, :4].view(torch.uint8), x[0].view(torch.uint8))
+
+
+# --- pages -------------------------------------------------------------------------
+
+
+def fork_state(g, n_in, ld, ps, pages, share):
+    lens = g.integers(0, ld * ps, n_in)
+    lens[g.random(n_in) < 0.2] = 0
+    lens[g.random(n_in) < 0.3] //= ps
+    lens[g.random(n_in) < 0.3] *= 1
+    table = np.full((n_in, ld), -1, np.int64)
+    ids = list(g.permutation(pages))
+    for s in range(n_in):
+        for j in range(-(-int(lens[s]) // ps)):
+            if s and g.random() < share and table[s - 1, j] >= 0:
+                table[s, j] = table[s - 1, j]
+            elif ids:
+                table[s, j] = ids.pop()
+            else:
+                lens[s] = j * ps
+                break
+    return table, lens
+
+
+def same_bits(a, b):
+    return torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "int4"])
+def test_fork_against_the_definition(cache):
+    g = np.random.default_rng(11)
+    refused = copied = 0
+    for trial in range(60):
+        ps = int(g.choice([16, 32]))
+        n_in, ld = int(g.integers(1, 40)), int(g.integers(1, 7))
+        pages = int(g.integers(2, n_in * ld + 30))
+        table, lens = fork_state(g, n_in, ld, ps, pages, g.choice([0.0, 0.5, 0.9]))
+        n_out = int(g.integers(1, 60))
+        parents = g.integers(-2 if trial % 3 else 0, n_in + (1 if trial % 5 == 0 else 0), n_out)
+        grow = trial % 4 != 3
+        if trial % 7 == 6:
+            table[g.integers(0, n_in), g.integers(0, ld)] = pages + 5
+            lens[g.integers(0, n_in)] = ld * ps + 100
+        pool = Pool(g, cache, 2, pages, ps, 2, 16)
+        before = {n: t.clone() for n, t in pool.tensors().items()}
+        r = pool.cache.fork(i32(table), i32(lens), i32(parents), grow=grow)
+        new, ln, refs, st, cp = R.fork(table, lens, parents, pages, ps, grow)
+        np.testing.assert_array_equal(host(r.table), new)
+        np.testing.assert_array_equal(host(r.lens), ln)
+        np.testing.assert_array_equal(host(r.refs), refs)
+        assert r.status.tolist() == st
+        for n, t in before.items():
+            for a, b in cp:
+                t[:, b] = t[:, a]
+            assert same_bits(t, pool.tensors()[n])
+        refused += st[0] > 0
+        copied += len(cp)
+    assert refused > 3 and copied > 50
+
+
+def test_fork_of_many_sequences_and_pages():
+    g = np.random.default_rng(12)
+    for n_in, ld, pages, n_out in ((3000, 4, 9000, 3100), (40, 300, 70001, 200), (1, 1, 1, 1)):
+        table, lens = fork_state(g, n_in, ld, 16, pages, 0.5)
+        parents = g.integers(-1, n_in, n_out)
+        cache = pdec.PagedCache("int4", 1, pages, 16, 1, 16)
+        r = cache.fork(i32(table), i32(lens), i32(parents))
+        new, ln, refs, st, cp = R.fork(table, lens, parents, pages, 16, True)
+        np.testing.assert_array_equal(host(r.table), new)
+        np.testing.assert_array_equal(host(r.lens), ln)
+        np.testing.assert_array_equal(host(r.refs), refs)
+        assert r.status.tolist() == st
+        m = cache.compact(i32(table), i32(lens))
+        new, remap, st, mv = R.compact(table, lens, pages, 16)
+        np.testing.assert_array_equal(host(m.table), new)
+        np.testing.assert_array_equal(host(m.remap), remap)
+        assert m.status.tolist() == st
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "int4"])
+def test_compaction_against_the_definition(cache):
+    g = np.random.default_rng(13)
+    moved = 0
+    for trial in range(25):
+        n, ld, ps = int(g.integers(1, 30)), int(g.integers(1, 6)), 16
+        pages = int(g.integers(2, 2 * n * ld + 10))
+        table, lens = fork_state(g, n, ld, ps, pages, 0.4)
+        if trial % 5 == 4:
+            table[0, 0], lens[0] = pages, ld * ps + 9
+        pool = Pool(g, cache, 3, pages, ps, 1, 32)
+        before = {k: t.clone() for k, t in pool.tensors().items()}
+        r = pool.cache.compact(i32(table), i32(lens))
+        new, remap, st, mv = R.compact(table, np.minimum(lens, ld * ps), pages, ps)
+        np.testing.assert_array_equal(host(r.table), new)
+        np.testing.assert_array_equal(host(r.remap), remap)
+        assert r.status.tolist() == st
+        for k, t in before.items():
+            for a, b in mv:
+                t[:, b] = t[:, a]
+            assert same_bits(t, pool.tensors()[k])
+        moved += len(mv)
+    assert moved > 50
+
+
+# --- selection -----------------------------------------------------------------------
+
+
+def run_select(logits, scores, lens, done, **kw):
+    return pdec.beam_select(logits, gpu(scores, torch.float32), i32(lens), i32(done), **kw)
+
+
+def check_select(r, logits, scores, lens, done, *, eos_id=2, pad_id=0, alpha=1.0, max_len=None):
+    S, par, tok, ln, dn, src, fl = R.select(host(logits), np.float32(scores).astype(np.float64), lens, done, eos_id, pad_id,
+                                            alpha, max_len)
+    for name, want in (("parents", par), ("tokens", tok), ("lens", ln), ("done", dn), ("src", src), ("flags", fl)):
+        np.testing.assert_array_equal(host(getattr(r, name)), want, err_msg=name)
+    got = host(r.scores)
+    there = S > -np.inf
+    assert (got[~there] == -np.inf).all()
+    # one rounding to float; the log-sum-exp's own error: exponentials to 2^-22
+    assert (np.abs(got[there] - S[there]) <= np.abs(S[there]) * U + 2.0 ** -22).all()
+
+
+SELECT = [(1, 4, 1000, "f32"), (3, 5, 1001, "bf16"), (2, 1, 999, "f32"), (2, 5, 58101, "f32"), (1, 5, 250027, "bf16"),
+          (7, 16, 4003, "f32"), (1, 64, 1111, "f32"), (2, 64, 130, "bf16"), (3, 4, 1, "f32"), (2, 6, 3, "f32"),
+          (1, 3, 1 << 20, "bf16"), (40, 2, 517, "f32"), (1, 33, 20011, "f32"), (300, 4, 64, "bf16"), (1, 1, 1, "bf16")]
+
+
+@pytest.mark.parametrize("B,K,V,dtype", SELECT)
+def test_selection_against_64_bits(B, K, V, dtype):
+    say("select", B, K, V, dtype)
+    g = np.random.default_rng(V + K)
+    for alpha, first in ((1.0, False), (0.6, False), (0.0, True)):
+        x = gpu(3 * g.normal(size=(B, K, V)), TYPES[dtype])
+        scores = -g.random((B, K)) * 20
+        lens = g.integers(1, 30, (B, K))
+        done = (g.random((B, K)) < 0.25).astype(int)
+        lens[done == 0] = 30
+        limit = g.integers(30, 33, B)
+        if first:                                              # a first step: one live beam
+            scores[:, 1:], scores[:, 0], lens[:], done[:] = -np.inf, 0, 0, 0
+        r = run_select(x, scores, lens, done, alpha=alpha, max_len=i32(limit))
+        check_select(r, x, scores, lens, done, alpha=alpha, max_len=limit)
+
+
+def test_selection_orders_of_logits():
+    """Rows in rising and falling order, all equal, with few levels, and with all that is large in one place."""
+    g = np.random.default_rng(21)
+    for V in (700, 9001):
+        i = np.arange(V)
+        rows = [i * 1e-3, -i * 1e-3, 0 * i, -0.0 * i, i // 100, -(i // 7), (i % 64 == 5) * 9.0, np.where(i >= V - 40, 5.0, -5.0),
+                np.where(i % 2, 0.0, -0.0), g.integers(0, 4, V), -1e30 * (i % 3), 1e30 * (i % 3), np.where(i == V - 1, 1e4, 0.0)]
+        for K in (1, 5, 16):
+            x = gpu(np.stack([np.stack([r] * K) for r in rows]), torch.float32)
+            x[:, K // 2] += 0.25                               # the same order, another log-sum-exp
+            B = len(rows)
+            scores = np.tile(-np.arange(K) * 0.5, (B, 1))
+            lens, done = np.full((B, K), 3), np.zeros((B, K), int)
+            for dt in (torch.float32, torch.bfloat16):
+                r = run_select(x.to(dt), scores, lens, done, alpha=0.0)
+                check_select(r, x.to(dt), scores, lens, done, alpha=0.0)
+
+
+def test_selection_of_logits_that_are_not_finite():
+    g = np.random.default_rng(22)
+    B, K, V = 6, 4, 2003
+    x = 3 * g.normal(size=(B, K, V))
+    x[0, 1, 17], x[1, 2, 100:300], x[2] = np.nan, np.inf, -np.inf
+    x[3, :, 5:] = -np.inf
+    x[4, 0], x[4, 1, ::2] = np.nan, -np.inf
+    x[5, 3, 2002] = np.nan                                     # a finished beam: not read
+    scores, lens, done = -g.random((B, K)) * 5, np.full((B, K), 4), np.zeros((B, K), int)
+    done[5, 3] = 1
+    scores[5, 0] = -np.inf
+    for dt in (torch.float32, torch.bfloat16):
+        t = gpu(x, dt)
+        r = run_select(t, scores, lens, done)
+        check_select(r, t, scores, lens, done)
+        assert r.flags.tolist() == [8, 8, 0, 0, 8, 0]
+
+
+def test_selection_strides_alignment_and_places():
+    g = np.random.default_rng(23)
+    B, K, V = 3, 5, 1003
+    scores, lens, done = -g.random((B, K)) * 5, np.full((B, K), 4), np.zeros((B, K), int)
+    done[1, 2] = 1
+    for dt in (torch.float32, torch.bfloat16):
+        for off in range(9):
+            wide = gpu(3 * g.normal(size=(B, K, V + 40)), dt)
+            x = wide[:, :, off:off + V]                        # rows of another distance, at every alignment
+            wide[:, :, :off] = 99.0                            # what lies beside a row is never taken
+            wide[:, :, off + V:] = 99.0
+            check_select(run_select(x, scores, lens, done), x, scores, lens, done)
+        narrow = gpu(3 * g.normal(size=(B, K, 3)), dt)
+        check_select(run_select(narrow, scores, lens, done), narrow, scores, lens, done)
+    # in place: scores, lengths and done are the outputs' own arrays
+    L = pdec.load_library()
+    x = gpu(3 * g.normal(size=(B, K, V)), torch.float32)
+    s, n, d = gpu(scores, torch.float32), i32(lens), i32(done)
+    want = pdec.beam_select(x, s, n, d)
+    o = torch.empty(3, B, K, dtype=torch.int32, device="cuda")
+    fl, ws = torch.empty(B, dtype=torch.int32, device="cuda"), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    assert L.pd_beam_select(x.data_ptr(), 0, V, B, K, V, s.data_ptr(), n.data_ptr(), d.data_ptr(), None, 2, 0, 1.0,
+                            s.data_ptr(), o[0].data_ptr(), o[1].data_ptr(), n.data_ptr(), d.data_ptr(), o[2].data_ptr(),
+                            fl.data_ptr(), ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream) == 0
+    for a, b in zip((s, o[0], o[1], n, d, o[2], fl), want):
+        assert torch.equal(a, b)
+
+
+# --- as they are used together, on streams and in graphs ----------------------------------
+
+
+def beam_program(g, cache, B, K, V, H, dh, ps, steps):
+    """A toy decoder: a word's key, value and query are rows of tables, the logits a product of the attention output.
+    Returns what a program keeps and one step of it."""
+    ld = steps // ps + 1
+    S = B * K
+    pool = pdec.PagedCache(cache, 1, S * ld + S, ps, H, dh)
+    w = {n: gpu(g.normal(size=(V, H, dh)), torch.float32) for n in "qkv"}
+    out = gpu(g.normal(size=(H * dh, V)) * (2.0 / math.sqrt(H * dh)), torch.float32)
+    bias = gpu(np.where(np.arange(V) == 2, 2.5, 0.0), torch.float32)        # [EOS] is likely
+    limit = i32(steps - 9 * np.arange(B))
+    st = {"scores": gpu(np.where(np.arange(K) == 0, 0.0, -np.inf)[None].repeat(B, 0), torch.float32),
+          "lens": torch.zeros((B, K), dtype=torch.int32, device="cuda"), "done": torch.zeros((B, K), dtype=torch.int32, device="cuda"),
+          "tok": torch.ones((B, K), dtype=torch.int32, device="cuda"), "table": torch.full((S, ld), -1, dtype=torch.int32, device="cuda"),
+          "n": torch.zeros(S, dtype=torch.int32, device="cuda"), "src": torch.arange(S, dtype=torch.int32, device="cuda")}
+
+    def step(st):
+        f = pool.fork(st["table"], st["n"], st["src"].reshape(-1))
+        t = st["tok"].reshape(-1).long()
+        o = pool.attend(w["q"][t], f.table, f.lens, group=K, new_k=w["k"][t], new_v=w["v"][t], out_dtype=torch.float32)
+        logits = (o.reshape(S, -1) @ out + bias).reshape(B, K, V)
+        r = pdec.beam_select(logits, st["scores"], st["lens"], st["done"], alpha=0.7, max_len=limit)
+        return {"scores": r.scores, "lens": r.lens, "done": r.done, "tok": r.tokens, "table": f.table, "n": f.lens,
+                "src": r.src, "par": r.parents, "logits": logits, "status": f.status}
+
+    return st, step, {n: host(x) for n, x in w.items()}, host(out), host(bias), host(limit)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "int4"])
+def test_the_operators_together(cache):
+    """Beam search of a toy decoder: every step's logits equal those of the hypotheses' whole histories, kept on the host."""
+    B, K, V, H, dh, ps, steps = 3, 4, 50, 2, 32, 16, 40
+    st, step, w, out, bias, limit = beam_program(np.random.default_rng(31), cache, B, K, V, H, dh, ps, steps)
+    hist = [[1] for _ in range(B * K)]
+
+    def held(x):
+        if cache == "int4":
+            return R.dequantise(*R.quantise(x))
+        return torch.from_numpy(x).to(TYPES[cache]).double().numpy()
+
+    wk, wv = held(w["k"]), held(w["v"])
+    ends = 0
+    for i in range(steps):
+        src, old = host(st["src"]).reshape(-1), st
+        st = step(st)
+        assert st["status"][0].item() == 0
+        assert host(st["n"]).tolist() == [len(h) if p >= 0 else 0 for h, p in zip(hist, src)]
+        logits = host(st["logits"]).reshape(B * K, V)
+        for s, h in enumerate(hist):
+            ref = (R.attend(w["q"][h[-1]], wk[h], wv[h], dh ** -0.5)[0].reshape(-1) if src[s] >= 0 else np.zeros(H * dh)) @ out + bias
+            # float attention and product: a few thousand roundings of values below 10
+            np.testing.assert_allclose(logits[s], ref, atol=2e-3)
+        check_select_step(st, logits.reshape(B, K, V), old, 0.7, limit)
+        par, tok = host(st["par"]), host(st["tok"])
+        hist = [hist[b * K + par[b, k]] + [int(tok[b, k])] if par[b, k] >= 0 else [1] for b in range(B) for k in range(K)]
+        ends += int(host(st["done"]).sum()) if i < steps - 9 * B else 0
+    assert ends > 0                                            # some hypotheses end before the others
+
+
+def check_select_step(st, logits, old, alpha, limit):
+    _, par, tok, _, _, src, _ = R.select(logits, host(old["scores"]), host(old["lens"]), host(old["done"]), 2, 0, alpha, limit)
+    np.testing.assert_array_equal(host(st["par"]), par)
+    np.testing.assert_array_equal(host(st["tok"]), tok)
+    np.testing.assert_array_equal(host(st["src"]), src)
+
+
+def test_a_step_in_a_graph_equals_eager_steps():
+    """One step captured on a stream and replayed, with eager steps of the same program between the replays."""
+    B, K, V, H, dh, ps, steps = 2, 5, 300, 4, 64, 16, 20
+    make = lambda: beam_program(np.random.default_rng(32), "bf16", B, K, V, H, dh, ps, steps)  # noqa: E731
+    st_e, step_e = make()[:2]
+    st_g, step_g = make()[:2]
+    step_g(st_g)                                               # warm up
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        res = step_g(st_g)
+    for i in range(6):
+        st_e = step_e(st_e)
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in ("scores", "tok", "src", "table", "n", "done", "logits"):
+            assert torch.equal(st_e[n].reshape(-1), res[n].reshape(-1)), (i, n)
+        for n in st_g:
+            st_g[n].copy_(res[n].reshape(st_g[n].shape))
+
+
+def test_calls_on_another_stream():
+    g = np.random.default_rng(33)
+    pool = Pool(g, "int4", 1, 64, 16, 4, 64)
+    lens = [200, 100, 50, 180]
+    table = tree_tables(g, lens, 1, 16, 64, False, 13)
+    q = gpu(g.normal(size=(4, 8, 64)), torch.float32)
+    x = gpu(3 * g.normal(size=(4, 1, 40001)), torch.float32)
+    z = torch.zeros(4, 1, device="cuda")
+    i = torch.zeros(4, 1, dtype=torch.int32, device="cuda")
+    t, n, par = i32(table), i32(lens), i32([0, 1, 2, 3])
+    want = (pool.cache.attend(q, t, n), pdec.beam_select(x, z, i, i).tokens)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):                                          # two streams at once, results of their own
+        a = [(pool.cache.attend(q, t, n, stream=s), pdec.beam_select(x, z, i, i, stream=s).tokens) for s in (s1, s2)]
+        f = pool.cache.fork(t, n, par, grow=False, stream=s1)
+        torch.cuda.synchronize()
+        for got in a:
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert torch.equal(f.table, t) and torch.equal(f.lens, n)
+
+
+def test_results_do_not_change_from_call_to_call():
+    g = np.random.default_rng(34)
+    pool = Pool(g, "bf16", 1, 800, 16, 8, 64)
+    lens = [int(n) for n in g.integers(1, 200, 40)]
+    table = tree_tables(g, lens, 5, 16, 800, True, 13)
+    q = gpu(g.normal(size=(40, 8, 64)), torch.float32)
+    x = gpu(3 * g.normal(size=(8, 5, 30011)), torch.bfloat16)
+    s, i = gpu(-g.random((8, 5)), torch.float32), torch.zeros(8, 5, dtype=torch.int32, device="cuda")
+    other = Pool(g, "bf16", 1, 800, 16, 8, 64)                 # a fork reuses the pages of sequences that end
+    first = None
+    for _ in range(5):
+        got = (pool.cache.attend(q, i32(table), i32(lens), group=5), *pdec.beam_select(x, s, i, i),
+               *other.cache.fork(i32(table), i32(lens), i32(np.arange(40) // 2)))
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(got, first))
