@@ -5,7 +5,10 @@
 // with k_j, v_j the key and value of head h / (heads / kv_heads) in slot
 // j mod page_size of page table[s][j / page_size].  Keys of pages that do not
 // exist (an id outside the pool) are left out; a row without keys is zero.
+#include <type_traits>
+
 #include "common.h"
+#include "mma.h"
 #include "operators.h"
 
 namespace pdec {
@@ -71,95 +74,567 @@ __device__ __forceinline__ uint32_t group_code(float x, float step, float least)
   return static_cast<uint32_t>(fminf(fmaxf(c, 0.f), 15.f));
 }
 
-// One thread per (sequence, head): its token at position len - 1.
-__global__ __launch_bounds__(64) void k_append(AttendArgs a) {
+// --- the tile ------------------------------------------------------------------
+//
+// A workgroup takes up to 16 query rows that read the same key/value head: the
+// beams of a group (RB of them) times the G query heads of the key head, and a
+// range of key blocks of 32 positions.  For each block it finds the distinct
+// (pages, valid keys) among its beams: beams that share a prefix share one
+// item, so a page is read once however many of them refer to it.  Waves take
+// items in turn; an item's keys are scored against all 16 rows on the matrix
+// cores (16x16 tiles: rows are keys, columns are queries) and only the rows
+// that own the item take the result.
+//
+// Key kappa of a block sits in row 4 (kappa / 8) + kappa % 4 of score tile
+// (kappa / 4) % 2, so that lane (n, g) = (lane % 16, lane / 16) ends up with the
+// scores of keys 8 g .. 8 g + 7 for query n, in the order in which the product
+// with V wants its weights: eight consecutive keys a lane, and V's pages hold
+// the keys of a dimension next to each other.
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kBlock = 32;                    // keys of an item
+constexpr int kListBlocks = 64;               // blocks whose items are listed at a time
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct Item {
+  int id0, id1;                               // pages of the block's halves (-1: none)
+  int block;
+  uint32_t rows_nv;                           // beams that own it (bits 16 ..), valid keys (low bits)
+};
+
+__device__ __forceinline__ float xor16_max(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float xor32_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float xor16_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float xor32_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ floatx4_t mma_bf16(uint4 a, uint4 b, floatx4_t c) { return Mma<bf16_t>::step(a, b, c); }
+__device__ __forceinline__ floatx4_t mma_f32(float a, float b, floatx4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+// Eight floats as bfloat16 parts: v = hi + lo (+ lo2) to 2^-17 (2^-25) of v.
+__device__ __forceinline__ uint4 pack8(const float* v) {
+  return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+}
+__device__ __forceinline__ void take_off(float* v, uint4 p) {   // v -= p
+  const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] -= __uint_as_float(w[j] << 16);
+    v[2 * j + 1] -= __uint_as_float(w[j] & 0xffff0000u);
+  }
+}
+
+// The eight codes of a word as bfloat16 16 + code: a code fills the top of the
+// mantissa of 16 (exact), two of them an instruction.  The offset and half the
+// code range are taken off inside the matrix product (kCodeMid), so that what
+// is accumulated is code - 7.5.
+__device__ __forceinline__ uint4 codes_bf16(uint32_t w) {
+  constexpr uint32_t m = 0x00780078u, e = 0x41804180u;
+  return make_uint4(((w << 3) & m) | e, ((w >> 1) & m) | e, ((w >> 5) & m) | e, ((w >> 9) & m) | e);
+}
+constexpr float kCodeMid = 7.5f;
+constexpr uint32_t kMinusMid2 = 0xc1bcc1bcu;   // two bfloat16 of -(16 + 7.5)
+
+// The tokens at position len - 1 of the tile's beams, where that lies in keys
+// [from, to): eight dimensions a lane.  In 4 bits a group's extremes come from
+// the four lanes that hold it.  The slots belong to one sequence each, so the
+// words that hold several tokens are read, changed and written by one lane.
+template <int CT, int DH>
+__device__ __forceinline__ void append_rows(const AttendArgs& a, int kv, int seq0, int beams, const int* s_len, int from,
+                                            int to) {
   const CacheView& c = a.c;
-  const long long i = blockIdx.x * 64ll + threadIdx.x;
-  if (i >= static_cast<long long>(a.n_seqs) * c.kv_heads) return;
-  const int s = static_cast<int>(i / c.kv_heads), h = static_cast<int>(i - static_cast<long long>(s) * c.kv_heads);
-  const int n = keys_of(a.lens, s, a.max_len, a.table_ld, c.ps);
-  if (n == 0) return;
-  const int t = (n - 1) % c.ps, id = page_at(a.table, a.table_ld, s, (n - 1) / c.ps, c.pages);
-  if (id < 0) return;
-  const size_t hb = head_block(c, a.layer, id, h);
-  for (int is_v = 0; is_v < 2; ++is_v) {
-    const void* x = is_v ? a.new_v : a.new_k;
-    const size_t x0 = static_cast<size_t>(s) * a.new_ld + static_cast<size_t>(h) * c.dh;
-    char* base = is_v ? c.v : c.k;
-    const int per = c.dh / c.groups;
-    for (int g = 0; g < c.groups; ++g) {
-      float step = 0.f, least = 0.f;
-      if (c.type == CT_INT4) {
-        float lo = INFINITY, hi = -INFINITY;
-        bool fin = true;
-        for (int d = g * per; d < (g + 1) * per; ++d) {
-          const float v = load_any(x, a.new_bf16, x0 + d);
-          lo = fminf(lo, v);
-          hi = fmaxf(hi, v);
-          fin = fin && isfinite(v);
-        }
-        group_params(lo, hi, fin, step, least);
-        reinterpret_cast<uint32_t*>(is_v ? c.vs : c.ks)[(hb * c.ps + t) * c.groups + g] =
-            (__float_as_uint(step) >> 16) | (__float_as_uint(least) & 0xffff0000u);
+  constexpr int L8 = DH / 8;
+  constexpr int G = DH >= 32 ? DH / 32 : 1;
+  for (int i0 = 0; i0 < beams * 2 * L8; i0 += kThreads) {
+    const int i = i0 + threadIdx.x;
+    const int r = i / (2 * L8), is_v = i / L8 & 1, d = 8 * (i & (L8 - 1));
+    const int pos = r < beams ? s_len[r] - 1 : -1;
+    const int id = pos >= from && pos < to ? page_at(a.table, a.table_ld, seq0 + r, pos / c.ps, c.pages) : -1;
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+    if (id >= 0) {
+      const void* src = is_v ? a.new_v : a.new_k;
+      const size_t x0 = static_cast<size_t>(seq0 + r) * a.new_ld + static_cast<size_t>(kv) * DH + d;
+      if (a.new_bf16) Vec16<bf16_t>::load(static_cast<const bf16_t*>(src), x0, x);
+      else load_n<float, 8>(static_cast<const float*>(src), x0, x);
+    }
+    float step = 0.f, least = 0.f;
+    if constexpr (CT == CT_INT4) {
+      float lo = x[0], hi = x[0], bad = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        lo = fminf(lo, x[e]);
+        hi = fmaxf(hi, x[e]);
+        bad = isfinite(x[e]) ? bad : 1.f;
       }
-      for (int d = g * per; d < (g + 1) * per; ++d) {
-        const float v = load_any(x, a.new_bf16, x0 + d);
-        const size_t o = hb * c.ps * c.dh + (is_v ? static_cast<size_t>(d) * c.ps + t : static_cast<size_t>(t) * c.dh + d);
-        if (c.type == CT_F32) {
-          reinterpret_cast<float*>(base)[o] = v;
-        } else if (c.type == CT_BF16) {
-          reinterpret_cast<bf16_t*>(base)[o] = f32_to_bf16(v);
+      lo = fminf(lo, dpp_f<kDppXor1>(lo)); hi = fmaxf(hi, dpp_f<kDppXor1>(hi)); bad = fmaxf(bad, dpp_f<kDppXor1>(bad));
+      if constexpr (DH >= 32) {
+        lo = fminf(lo, dpp_f<kDppXor2>(lo)); hi = fmaxf(hi, dpp_f<kDppXor2>(hi)); bad = fmaxf(bad, dpp_f<kDppXor2>(bad));
+      }
+      group_params(lo, hi, bad == 0.f, step, least);
+    }
+    if (id < 0) continue;
+    const size_t hb = head_block(c, a.layer, id, kv);
+    const int t = pos & (c.ps - 1);
+    char* base = is_v ? c.v : c.k;
+    const size_t row = (hb * c.ps + t) * DH + d;            // K
+    if constexpr (CT == CT_INT4) {
+      uint32_t code[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) code[e] = group_code(x[e], step, least);
+      if (d % 32 == 0)
+        reinterpret_cast<uint32_t*>(is_v ? c.vs : c.ks)[(hb * c.ps + t) * G + d / 32] =
+            (__float_as_uint(step) >> 16) | (__float_as_uint(least) & 0xffff0000u);
+      uint32_t* w = reinterpret_cast<uint32_t*>(base);
+      if (!is_v) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) word |= code[e] << nibble_shift(e);
+        w[row >> 3] = word;
+      } else {
+        const int sh = nibble_shift(t & 7);
+        uint32_t old[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) old[e] = w[((hb * DH + d + e) * c.ps + t) >> 3];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[((hb * DH + d + e) * c.ps + t) >> 3] = (old[e] & ~(15u << sh)) | (code[e] << sh);
+      }
+    } else {
+      typedef typename std::conditional<CT == CT_F32, float, bf16_t>::type T;
+      T* w = reinterpret_cast<T*>(base);
+      if (!is_v) {
+        store8<T>(w, row, x);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) Elt<T>::store(w, (hb * DH + d + e) * c.ps + t, x[e]);
+      }
+    }
+  }
+  __threadfence_block();
+}
+
+// out = o / l for four dimensions of a row; a row without keys is zero.
+__device__ __forceinline__ void store_out(const AttendArgs& a, int s, int h, int d, const floatx4_t& o, float l) {
+  const float inv = l != 0.f ? 1.f / l : 0.f;      // NaN stays
+  const size_t at = static_cast<size_t>(s) * a.out_ld + static_cast<size_t>(h) * a.c.dh + d;
+  if (a.out_bf16) {
+    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + at) =
+        make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+  } else {
+    *reinterpret_cast<floatx4_t*>(static_cast<float*>(a.out) + at) = floatx4_t{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  }
+}
+
+// Split of the launch: beams per tile, tiles of a group, ranges of the keys.
+struct Plan {
+  int rows_per_tile, tiles, splits, blocks_per_split;
+};
+
+template <int CT, int DH>
+__global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
+  constexpr int NU = DH >= 32 ? DH / 32 : 1;          // steps of 32 dimensions (bf16 products), groups of a cache in 4 bits
+  constexpr int NT = DH / 16;                         // tiles of 16 dimensions
+  constexpr int NF = CT == CT_F32 ? DH / 16 : 1;      // float: steps of 16 dimensions
+  const CacheView& c = a.c;
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int n = lane & 15, g = lane >> 4;
+  const int G = a.heads / c.kv_heads;
+  int wg = blockIdx.x;
+  const int split = wg % pl.splits; wg /= pl.splits;
+  const int kv = wg % c.kv_heads; wg /= c.kv_heads;
+  const int tile = wg % pl.tiles;
+  const int grp = wg / pl.tiles;
+  const int beam0 = tile * pl.rows_per_tile;
+  const int beams = min(pl.rows_per_tile, a.group - beam0);
+  const int seq0 = grp * a.group + beam0;
+  const int ps = c.ps;
+
+  __shared__ Item s_item[kListBlocks * 16];
+  __shared__ int4 s_tup[kListBlocks * 16];
+  __shared__ int s_len[16];
+  __shared__ int s_cnt[kWaves];
+  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  __shared__ float s_o[kWaves][16][DH + 4];
+
+  if (threadIdx.x < 16)
+    s_len[threadIdx.x] = static_cast<int>(threadIdx.x) < beams ? keys_of(a.lens, seq0 + threadIdx.x, a.max_len, a.table_ld, ps) : 0;
+  // queries: lane (n, g) holds dimensions 32 u + 8 g .. + 7 (float: 16 u + 4 g .. + 3) of row n
+  const int beam_n = n / G;
+  const bool row_ok = beam_n < beams;
+  const size_t q0 = static_cast<size_t>(seq0 + (row_ok ? beam_n : 0)) * a.q_ld +
+                    (static_cast<size_t>(kv) * G + (row_ok ? n % G : 0)) * DH;
+  const float s2 = a.scale * kLog2e;                  // scores in units of log 2
+  uint4 qf[CT == CT_F32 ? 1 : NU][3];
+  floatx4_t q32[NF];
+  float qsum[NU];                                     // 4 bits: sum of the row's queries over a group
+  floatx4_t qmid[NU];                                 // and -(16 + 7.5) times it
+  if constexpr (CT == CT_F32) {
+#pragma unroll
+    for (int u = 0; u < NF; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q32[u][e] = row_ok ? load_any(a.q, a.q_bf16, q0 + 16 * u + 4 * g + e) : 0.f;
+  } else {
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool in = row_ok && (DH >= 32 || g < 2);
+        v[e] = in ? load_any(a.q, a.q_bf16, q0 + 32 * u + 8 * g + e) : 0.f;
+      }
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += v[e];
+      qsum[u] = xor32_sum(xor16_sum(sum));
+#pragma unroll
+      for (int part = 0; part < 3; ++part) {
+        qf[u][part] = pack8(v);
+        take_off(v, qf[u][part]);
+      }
+      if constexpr (CT == CT_INT4) {
+        const uint4 mid = make_uint4(kMinusMid2, kMinusMid2, kMinusMid2, kMinusMid2);
+        qmid[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int part = 0; part < 3; ++part) qmid[u] = mma_bf16(mid, qf[u][part], qmid[u]);
+      }
+    }
+  }
+  __syncthreads();
+
+  int longest = 0;
+  for (int r = 0; r < beams; ++r) longest = max(longest, s_len[r]);
+  const int b_begin = split * pl.blocks_per_split;
+  const int b_end = min(b_begin + pl.blocks_per_split, (longest + kBlock - 1) / kBlock);
+
+  // the step's own token, by the workgroup whose range holds its position
+  if (a.new_k != nullptr) append_rows<CT, DH>(a, kv, seq0, beams, s_len, b_begin * kBlock, b_end * kBlock);
+
+  float m = -INFINITY, l = 0.f;
+  floatx4_t acc[NT];
+  float mid[NU];                                      // 4 bits: sum of p times the middle of a key's group, own keys
+#pragma unroll
+  for (int t = 0; t < NT; ++t) acc[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int u = 0; u < NU; ++u) mid[u] = 0.f;
+
+  for (int b0 = b_begin; b0 < b_end; b0 += kListBlocks) {
+    // --- the items of up to kListBlocks blocks ---
+    const int nb = min(kListBlocks, b_end - b0);
+    const int pairs = nb * beams;
+    __syncthreads();
+    for (int i = threadIdx.x; i < pairs; i += kThreads) {
+      const int b = i / beams, r = i - b * beams;
+      const int j0 = (b0 + b) * kBlock;
+      const int nv = max(0, min(kBlock, s_len[r] - j0));
+      const int s = seq0 + r;
+      int id0 = -1, id1 = -1;
+      if (nv > 0) id0 = page_at(a.table, a.table_ld, s, j0 / ps, c.pages);
+      if (nv > 16) id1 = ps > 16 ? id0 : page_at(a.table, a.table_ld, s, j0 / ps + 1, c.pages);
+      s_tup[i] = make_int4(id0, id1, nv, 0);
+    }
+    __syncthreads();
+    int n_items = 0;
+    for (int i0 = 0; i0 < pairs; i0 += kThreads) {
+      const int i = i0 + threadIdx.x;
+      bool lead = false;
+      Item it;
+      if (i < pairs) {
+        const int b = i / beams, r = i - b * beams;
+        const int4 t = s_tup[i];
+        lead = t.z > 0 && (t.x >= 0 || t.y >= 0);
+        uint32_t rows = 0;
+        for (int o = 0; o < beams; ++o) {
+          const int4 x = s_tup[b * beams + o];
+          const bool same = x.x == t.x && x.y == t.y && x.z == t.z;
+          rows |= same ? 1u << o : 0u;
+          if (same && o < r) lead = false;
+        }
+        it = Item{t.x, t.y, b0 + b, rows << 16 | static_cast<uint32_t>(t.z)};
+      }
+      const uint64_t vote = __ballot(lead);
+      if (lane == 0) s_cnt[wave] = __popcll(vote);
+      __syncthreads();
+      int at = n_items;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        at += w < wave ? s_cnt[w] : 0;
+        n_items += s_cnt[w];
+      }
+      if (lead) s_item[at + __popcll(vote & ((1ull << lane) - 1))] = it;
+      __syncthreads();
+    }
+
+    for (int i = wave; i < n_items; i += kWaves) {
+      const Item it = s_item[i];
+      const int nv = it.rows_nv & 0xffff;
+      const bool own = row_ok && ((it.rows_nv >> 16) >> beam_n & 1u);
+      const int j0 = it.block * kBlock;
+      const bool whole = nv == kBlock && it.id0 >= 0 && it.id1 >= 0;
+      // head blocks of the two halves (a missing page is never used: any block serves as its address)
+      const size_t hb0 = head_block(c, a.layer, max(it.id0, 0), kv), hb1 = head_block(c, a.layer, max(it.id1, 0), kv);
+      // --- loads ---
+      const size_t hb_v = g < 2 ? hb0 : hb1;            // of keys 8 g ..
+      const int slot_v = (j0 + 8 * g) & (ps - 1);
+      uint32_t k4[2][NU], v4[NT];
+      uint4 kf[2][CT == CT_BF16 ? NU : 1], vf[CT == CT_BF16 ? NT : 1];
+      floatx4_t k32[2][NF], v32[CT == CT_F32 ? NT : 1][2];
+      uint32_t kp[8][NU], vp[8][NU];                    // (step, least) of the lane's keys 8 g + j
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int kappa = 8 * (n >> 2) + 4 * t + (n & 3);
+        const size_t row = (kappa < 16 ? hb0 : hb1) * ps + ((j0 + kappa) & (ps - 1));
+        if constexpr (CT == CT_F32) {
+          const float* p = reinterpret_cast<const float*>(c.k) + row * DH + 4 * g;
+#pragma unroll
+          for (int u = 0; u < NF; ++u) k32[t][u] = *reinterpret_cast<const floatx4_t*>(p + 16 * u);
+        } else if constexpr (CT == CT_BF16) {
+          const bf16_t* p = reinterpret_cast<const bf16_t*>(c.k) + row * DH + (DH >= 32 ? 8 * g : 8 * (g & 1));
+#pragma unroll
+          for (int u = 0; u < NU; ++u) kf[t][u] = *reinterpret_cast<const uint4*>(p + 32 * u);
         } else {
-          uint32_t* w = reinterpret_cast<uint32_t*>(base) + (o >> 3);
-          const int sh = nibble_shift(static_cast<int>(o & 7));
-          *w = (*w & ~(15u << sh)) | (group_code(v, step, least) << sh);
+          const uint32_t* p = reinterpret_cast<const uint32_t*>(c.k) + row * (DH / 8) + (DH >= 32 ? g : (g & 1));
+#pragma unroll
+          for (int u = 0; u < NU; ++u) k4[t][u] = p[4 * u];
+        }
+      }
+      if constexpr (CT == CT_INT4) {
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(c.ks) + (hb_v * ps + slot_v) * NU;
+        const uint32_t* pv = reinterpret_cast<const uint32_t*>(c.vs) + (hb_v * ps + slot_v) * NU;
+#pragma unroll
+        for (int w = 0; w < 8 * NU; w += 4) {
+          const uint4 x = *reinterpret_cast<const uint4*>(p + w), y = *reinterpret_cast<const uint4*>(pv + w);
+          kp[w / NU][w % NU] = x.x; kp[(w + 1) / NU][(w + 1) % NU] = x.y;
+          kp[(w + 2) / NU][(w + 2) % NU] = x.z; kp[(w + 3) / NU][(w + 3) % NU] = x.w;
+          vp[w / NU][w % NU] = y.x; vp[(w + 1) / NU][(w + 1) % NU] = y.y;
+          vp[(w + 2) / NU][(w + 2) % NU] = y.z; vp[(w + 3) / NU][(w + 3) % NU] = y.w;
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const size_t at = (hb_v * DH + 16 * t + n) * ps + slot_v;
+        if constexpr (CT == CT_F32) {
+          v32[t][0] = *reinterpret_cast<const floatx4_t*>(reinterpret_cast<const float*>(c.v) + at);
+          v32[t][1] = *reinterpret_cast<const floatx4_t*>(reinterpret_cast<const float*>(c.v) + at + 4);
+        } else if constexpr (CT == CT_BF16) {
+          vf[t] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(c.v) + at);
+        } else {
+          v4[t] = reinterpret_cast<const uint32_t*>(c.v)[at >> 3];
+        }
+      }
+      // --- scores of keys 8 g + j, in units of log 2 ---
+      float sc[8];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        floatx4_t d = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (CT == CT_F32) {
+#pragma unroll
+          for (int u = 0; u < NF; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d = mma_f32(k32[t][u][e], q32[u][e], d);
+        } else if constexpr (CT == CT_BF16) {
+#pragma unroll
+          for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int part = 0; part < 3; ++part) d = mma_bf16(kf[t][u], qf[u][part], d);
+        } else {
+#pragma unroll
+          for (int u = 0; u < NU; ++u) {
+            floatx4_t x = qmid[u];
+            const uint4 w = codes_bf16(k4[t][u]);
+#pragma unroll
+            for (int part = 0; part < 3; ++part) x = mma_bf16(w, qf[u][part], x);
+#pragma unroll
+            for (int i2 = 0; i2 < 4; ++i2) {
+              const uint32_t pr = kp[4 * t + i2][u];
+              const float step = __uint_as_float(pr << 16), least = __uint_as_float(pr & 0xffff0000u);
+              d[i2] = fmaf(fmaf(kCodeMid, step, least), qsum[u], fmaf(step, x[i2], d[i2]));
+            }
+          }
+        }
+#pragma unroll
+        for (int i2 = 0; i2 < 4; ++i2) sc[4 * t + i2] = d[i2] * s2;
+      }
+      uint32_t live = 0xff;                             // keys of this lane that exist
+      if (!whole) {
+        const int here = (g < 2 ? it.id0 : it.id1) >= 0 ? max(0, min(8, nv - 8 * g)) : 0;
+        live = (1u << here) - 1u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sc[j] = (live >> j & 1u) ? sc[j] : -INFINITY;
+      }
+      // --- running softmax ---
+      float mx = fmaxf(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])), fmaxf(fmaxf(sc[4], sc[5]), fmaxf(sc[6], sc[7])));
+      mx = xor32_max(xor16_max(mx));
+      const float mn = fmaxf(m, mx);
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      float p[8], sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        p[j] = (live >> j & 1u) ? __builtin_amdgcn_exp2f(sc[j] - mn) : 0.f;
+        sum += p[j];
+      }
+      // --- weights times V ---
+      floatx4_t o[NT];
+      float om[NU];
+      if constexpr (CT == CT_F32) {
+        if (!whole) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v32[t][j >> 2][j & 3] = (live >> j & 1u) ? v32[t][j >> 2][j & 3] : 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          o[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[t] = mma_f32(v32[t][j >> 2][j & 3], p[j], o[t]);
+        }
+      } else if constexpr (CT == CT_BF16) {
+        if (!whole) {
+          uint32_t mk[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            mk[j] = ((live >> (2 * j) & 1u) ? 0xffffu : 0u) | ((live >> (2 * j + 1) & 1u) ? 0xffff0000u : 0u);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) vf[t] = make_uint4(vf[t].x & mk[0], vf[t].y & mk[1], vf[t].z & mk[2], vf[t].w & mk[3]);
+        }
+        const uint4 hi = pack8(p);
+        float r[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[j] = p[j];
+        take_off(r, hi);
+        const uint4 lo = pack8(r);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          o[t] = mma_bf16(vf[t], hi, floatx4_t{0.f, 0.f, 0.f, 0.f});
+          o[t] = mma_bf16(vf[t], lo, o[t]);
+        }
+      } else {
+        const uint4 off = make_uint4(kMinusMid2, kMinusMid2, kMinusMid2, kMinusMid2);
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+          float r[8];
+          om[u] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t pr = (whole || (live >> j & 1u)) ? vp[j][u] : 0u;
+            const float step = __uint_as_float(pr << 16), least = __uint_as_float(pr & 0xffff0000u);
+            r[j] = p[j] * step;
+            om[u] = fmaf(p[j], fmaf(kCodeMid, step, least), om[u]);
+          }
+          const uint4 hi = pack8(r);
+          take_off(r, hi);
+          const uint4 lo = pack8(r);
+          floatx4_t base = mma_bf16(off, hi, floatx4_t{0.f, 0.f, 0.f, 0.f});
+          base = mma_bf16(off, lo, base);
+#pragma unroll
+          for (int t = u * (NT / NU); t < (u + 1) * (NT / NU); ++t) {
+            const uint4 w = codes_bf16(v4[t]);
+            o[t] = mma_bf16(w, hi, base);
+            o[t] = mma_bf16(w, lo, o[t]);
+          }
+        }
+      }
+      if (own) {
+        l = fmaf(l, f, sum);
+        m = mn;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[t][e] = fmaf(acc[t][e], f, o[t][e]);
+        if constexpr (CT == CT_INT4) {
+#pragma unroll
+          for (int u = 0; u < NU; ++u) mid[u] = fmaf(mid[u], f, om[u]);
         }
       }
     }
   }
+
+  // --- the waves' parts ---
+  l = xor32_sum(xor16_sum(l));
+  if constexpr (CT == CT_INT4) {
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      const float x = xor32_sum(xor16_sum(mid[u]));
+#pragma unroll
+      for (int t = u * (NT / NU); t < (u + 1) * (NT / NU); ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[t][e] += x;
+    }
+  }
+  if (g == 0) {
+    s_m[wave][n] = m;
+    s_l[wave][n] = l;
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) *reinterpret_cast<floatx4_t*>(&s_o[wave][n][16 * t + 4 * g]) = acc[t];
+  __syncthreads();
+  const int rows = beams * G;
+  const int parts = a.n_seqs * a.heads;
+  for (int i = threadIdx.x; i < rows * (DH / 4); i += kThreads) {
+    const int r = i / (DH / 4), d = 4 * (i - r * (DH / 4));
+    float mt = s_m[0][r];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) mt = fmaxf(mt, s_m[w][r]);
+    float lt = 0.f;
+    floatx4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = s_m[w][r] == -INFINITY && !(s_l[w][r] != 0.f) ? 0.f : __builtin_amdgcn_exp2f(s_m[w][r] - mt);
+      lt = fmaf(s_l[w][r], f, lt);
+      const floatx4_t x = *reinterpret_cast<const floatx4_t*>(&s_o[w][r][d]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(x[e], f, o[e]);
+    }
+    const int s = seq0 + r / G, h = kv * G + r % G;
+    if (pl.splits == 1) {
+      store_out(a, s, h, d, o, lt);
+    } else {
+      const size_t part = static_cast<size_t>(split) * parts + static_cast<size_t>(s) * a.heads + h;
+      float* base = reinterpret_cast<float*>(a.ws);
+      *reinterpret_cast<floatx4_t*>(base + part * DH + d) = o;
+      if (d == 0) reinterpret_cast<float2*>(base + static_cast<size_t>(pl.splits) * parts * DH)[part] = make_float2(mt, lt);
+    }
+  }
 }
 
-constexpr int kAttnThreads = 64;
-
-// One wave per (sequence, head); a lane keeps its own running maximum, sum and
-// output over keys lane, lane + 64, ...
-__global__ __launch_bounds__(kAttnThreads) void k_attend(AttendArgs a) {
-  const CacheView& c = a.c;
-  const int s = blockIdx.x / a.heads, h = blockIdx.x % a.heads, lane = threadIdx.x;
-  const int kv = h / (a.heads / c.kv_heads);
-  const int n = keys_of(a.lens, s, a.max_len, a.table_ld, c.ps);
-  __shared__ float s_q[128];
-  __shared__ float s_o[kAttnThreads][129];
-  for (int d = lane; d < c.dh; d += kAttnThreads)
-    s_q[d] = load_any(a.q, a.q_bf16, static_cast<size_t>(s) * a.q_ld + static_cast<size_t>(h) * c.dh + d);
-  for (int d = 0; d < c.dh; ++d) s_o[lane][d] = 0.f;
-  __syncthreads();
-  float m = -INFINITY, l = 0.f;
-  for (int j = lane; j < n; j += kAttnThreads) {
-    const int id = page_at(a.table, a.table_ld, s, j / c.ps, c.pages);
-    if (id < 0) continue;
-    const size_t hb = head_block(c, a.layer, id, kv);
-    float dot = 0.f;
-    for (int d = 0; d < c.dh; ++d) dot = fmaf(s_q[d], cache_value(c, hb, j % c.ps, d, 0), dot);
-    const float sc = dot * a.scale, mn = fmaxf(m, sc);
-    const float f = m == -INFINITY ? 0.f : expf(m - mn), p = expf(sc - mn);
-    for (int d = 0; d < c.dh; ++d) s_o[lane][d] = fmaf(p, cache_value(c, hb, j % c.ps, d, 1), s_o[lane][d] * f);
-    l = l * f + p;
-    m = mn;
+// The parts of a row's key ranges, in their order: one lane per four dimensions.
+template <int DH>
+__global__ __launch_bounds__(256) void k_join(AttendArgs a, int splits) {
+  const long long i = blockIdx.x * 256ll + threadIdx.x;
+  const int parts = a.n_seqs * a.heads;
+  const long long row = i / (DH / 4);
+  if (row >= parts) return;
+  const int d = 4 * static_cast<int>(i - row * (DH / 4));
+  const float* base = reinterpret_cast<const float*>(a.ws);
+  const float2* ml = reinterpret_cast<const float2*>(base + static_cast<size_t>(splits) * parts * DH);
+  float mt = -INFINITY;
+  for (int z = 0; z < splits; ++z) mt = fmaxf(mt, ml[static_cast<size_t>(z) * parts + row].x);
+  float lt = 0.f;
+  floatx4_t o = {0.f, 0.f, 0.f, 0.f};
+  for (int z = 0; z < splits; ++z) {
+    const size_t part = static_cast<size_t>(z) * parts + row;
+    const float2 x = ml[part];
+    const float f = x.x == -INFINITY && !(x.y != 0.f) ? 0.f : __builtin_amdgcn_exp2f(x.x - mt);
+    lt = fmaf(x.y, f, lt);
+    const floatx4_t v = *reinterpret_cast<const floatx4_t*>(base + part * DH + d);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], f, o[e]);
   }
-  const float mx = wave_max(m);
-  const float f = m == -INFINITY ? 0.f : expf(m - mx);
-  const float sum = wave_sum(l * f);
-  for (int d = 0; d < c.dh; ++d) s_o[lane][d] *= f;
-  __syncthreads();
-  for (int d = lane; d < c.dh; d += kAttnThreads) {
-    float o = 0.f;
-    for (int i = 0; i < kAttnThreads; ++i) o += s_o[i][d];
-    o = sum > 0.f || sum != sum ? o / sum : 0.f;
-    const size_t at = static_cast<size_t>(s) * a.out_ld + static_cast<size_t>(h) * c.dh + d;
-    if (a.out_bf16) Elt<bf16_t>::store(static_cast<bf16_t*>(a.out), at, o);
-    else static_cast<float*>(a.out)[at] = o;
-  }
+  store_out(a, static_cast<int>(row / a.heads), static_cast<int>(row % a.heads), d, o, lt);
 }
 
 __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
@@ -188,17 +663,60 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
 
 }  // namespace
 
-size_t attend_workspace(const CacheView& c, int n_seqs, int heads, int group, int max_len) { return 0; }
+namespace {
+
+// Beams per tile: whole beams within 16 query rows.  Ranges of the keys: as many
+// as give the chip kWantWgs workgroups, while a range keeps two blocks for each
+// wave.
+constexpr int kWantWgs = 1024;
+Plan plan_attend(const CacheView& c, int n_seqs, int heads, int group, int max_len) {
+  Plan p;
+  const int G = heads / c.kv_heads;
+  p.rows_per_tile = 16 / G < group ? 16 / G : group;
+  p.tiles = (group + p.rows_per_tile - 1) / p.rows_per_tile;
+  const int blocks = (max_len + kBlock - 1) / kBlock;
+  const long long wgs = static_cast<long long>(n_seqs / group) * p.tiles * c.kv_heads;
+  long long want = (kWantWgs + wgs - 1) / wgs;
+  const long long most = (blocks + 2 * kWaves - 1) / (2 * kWaves);
+  if (want > most) want = most;
+  p.blocks_per_split = static_cast<int>((blocks + want - 1) / want);
+  p.splits = (blocks + p.blocks_per_split - 1) / p.blocks_per_split;
+  return p;
+}
+
+template <int CT, int DH>
+hipError_t launch_attend_t(const AttendArgs& a, const Plan& p, hipStream_t s) {
+  const long long wgs = static_cast<long long>(a.n_seqs / a.group) * p.tiles * a.c.kv_heads * p.splits;
+  hipLaunchKernelGGL((k_attend<CT, DH>), dim3(static_cast<unsigned>(wgs)), dim3(kThreads), 0, s, a, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const long long lanes = static_cast<long long>(a.n_seqs) * a.heads * (DH / 4);
+  hipLaunchKernelGGL(k_join<DH>, dim3(static_cast<unsigned>((lanes + 255) / 256)), dim3(256), 0, s, a, p.splits);
+  return hipGetLastError();
+}
+
+template <int CT>
+hipError_t launch_attend_ct(const AttendArgs& a, const Plan& p, hipStream_t s) {
+  switch (a.c.dh) {
+    case 16: return launch_attend_t<CT, 16>(a, p, s);
+    case 32: return launch_attend_t<CT, 32>(a, p, s);
+    case 64: return launch_attend_t<CT, 64>(a, p, s);
+    default: return launch_attend_t<CT, 128>(a, p, s);
+  }
+}
+
+}  // namespace
+
+size_t attend_workspace(const CacheView& c, int n_seqs, int heads, int group, int max_len) {
+  const Plan p = plan_attend(c, n_seqs, heads, group, max_len);
+  return p.splits == 1 ? 0 : static_cast<size_t>(p.splits) * n_seqs * heads * (c.dh * 4 + 8);
+}
 
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t s) {
-  if (a.new_k != nullptr) {
-    const long long n = static_cast<long long>(a.n_seqs) * a.c.kv_heads;
-    hipLaunchKernelGGL(k_append, dim3(static_cast<unsigned>((n + 63) / 64)), dim3(64), 0, s, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(k_attend, dim3(a.n_seqs * a.heads), dim3(kAttnThreads), 0, s, a);
-  return hipGetLastError();
+  const Plan p = plan_attend(a.c, a.n_seqs, a.heads, a.group, a.max_len);
+  if (a.c.type == CT_F32) return launch_attend_ct<CT_F32>(a, p, s);
+  if (a.c.type == CT_BF16) return launch_attend_ct<CT_BF16>(a, p, s);
+  return launch_attend_ct<CT_INT4>(a, p, s);
 }
 
 hipError_t launch_cache_read(const ReadArgs& a, hipStream_t s) {
