@@ -119,7 +119,7 @@ pd_status pd_beam_select_bytes(int32_t dtype, int32_t B, int32_t beam, int32_t v
   if (bytes == nullptr) return fail(PD_E_ARG, "null argument");
   const pd_status st = check_select(dtype, B, beam, vocab);
   if (st != PD_OK) return st;
-  *bytes = select_workspace(B, beam, vocab);
+  *bytes = select_workspace(dtype, B, beam, vocab);
   return PD_OK;
 }
 
@@ -137,7 +137,7 @@ pd_status pd_beam_select(const void* logits, int32_t dtype, int64_t ld, int32_t 
   if (ld < vocab || ld > (1LL << 40)) return fail(PD_E_ARG, "ld must be in [vocab, 2^40]");
   if (!aligned(logits, dtype == PD_BF16 ? 2 : 4)) return fail(PD_E_ARG, "logits are misaligned");
   if (!(alpha >= 0.f) || !std::isfinite(alpha)) return fail(PD_E_ARG, "alpha must be finite and >= 0");
-  if ((st = check_workspace(workspace, workspace_bytes, select_workspace(B, beam, vocab))) != PD_OK) return st;
+  if ((st = check_workspace(workspace, workspace_bytes, select_workspace(dtype, B, beam, vocab))) != PD_OK) return st;
   const SelectArgs a{logits, dtype, ld, B, beam, vocab, scores, lens, done, max_len, eos_id, pad_id, alpha,
                      out_scores, out_parent, out_token, out_len, out_done, out_src, out_flags,
                      static_cast<char*>(workspace)};

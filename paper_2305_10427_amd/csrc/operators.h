@@ -49,7 +49,7 @@ struct SelectArgs {
   int *out_parent, *out_token, *out_len, *out_done, *out_src, *out_flags;
   char* ws;
 };
-size_t select_workspace(int B, int beam, int vocab);
+size_t select_workspace(int dtype, int B, int beam, int vocab);
 hipError_t launch_beam_select(const SelectArgs& a, hipStream_t s);
 
 struct AttendArgs {

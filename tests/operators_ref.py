@@ -11,6 +11,33 @@ NONFINITE = 8
 # --- selection -------------------------------------------------------------------
 
 
+def candidates(logits, scores, lens, done, pad, alpha):
+    """A sentence's candidates (-key, beam, rank, score, token, length, finished), best first, and its flags."""
+    K, V = logits.shape
+    cands, flags = [], 0
+    for k in range(K):
+        s = float(scores[k])
+        if not math.isfinite(s):
+            continue
+        if done[k]:
+            cands.append((-s / max(int(lens[k]), 1) ** float(alpha), k, 0, s, pad, int(lens[k]), 1))
+            continue
+        x = np.array(logits[k], np.float64)
+        bad = np.isnan(x) | (x == np.inf)
+        flags |= NONFINITE * bool(bad.any())
+        x[bad] = -np.inf
+        words = np.nonzero(x > -np.inf)[0]
+        if not len(words):
+            continue
+        m = x.max()
+        lse = m + math.log(math.fsum(np.exp(x[words] - m)))
+        for r, v in enumerate(words[np.lexsort((words, -x[words]))][:K]):
+            c = s + (x[v] - lse)
+            n = int(lens[k]) + 1
+            cands.append((-c / max(n, 1) ** float(alpha), k, r, c, int(v), n, 0))
+    return sorted(cands, key=lambda c: c[:3]), flags
+
+
 def select(logits, scores, lens, done, eos, pad, alpha, max_len=None):
     """logits [B, K, V] float64; returns (scores f64, parents, tokens, lens, done, src, flags)."""
     B, K, V = logits.shape
@@ -19,28 +46,7 @@ def select(logits, scores, lens, done, eos, pad, alpha, max_len=None):
     par[:], tok[:], dn[:], src[:] = -1, pad, 1, -1
     flags = np.zeros(B, np.int32)
     for b in range(B):
-        cands = []
-        for k in range(K):
-            s = float(scores[b, k])
-            if not math.isfinite(s):
-                continue
-            if done[b, k]:
-                cands.append((-s / max(int(lens[b, k]), 1) ** float(alpha), k, 0, s, pad, int(lens[b, k]), 1))
-                continue
-            x = np.array(logits[b, k], np.float64)
-            bad = np.isnan(x) | (x == np.inf)
-            flags[b] |= NONFINITE * bool(bad.any())
-            x[bad] = -np.inf
-            words = np.nonzero(x > -np.inf)[0]
-            if not len(words):
-                continue
-            m = x.max()
-            lse = m + math.log(math.fsum(np.exp(x[words] - m)))
-            for r, v in enumerate(words[np.lexsort((words, -x[words]))][:K]):
-                c = s + (x[v] - lse)
-                n = int(lens[b, k]) + 1
-                cands.append((-c / max(n, 1) ** float(alpha), k, r, c, int(v), n, 0))
-        cands.sort(key=lambda c: c[:3])
+        cands, flags[b] = candidates(logits[b], scores[b], lens[b], done[b], pad, alpha)
         for j, (_, k, _, c, v, n, fin) in enumerate(cands[:K]):
             S[b, j], par[b, j], tok[b, j], ln[b, j] = c, k, v, n
             dn[b, j] = int(fin or v == eos or (max_len is not None and n >= max_len[b]))
