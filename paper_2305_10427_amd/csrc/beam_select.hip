@@ -14,8 +14,8 @@
 // above the complement of the word, so that a larger number is a better
 // candidate and equal logits go to the lower word, in whatever order a row is
 // read.  A wave keeps the bar (the beam-th best number so far) and collects
-// what is above it in LDS; the maximum of each lane's 16 bytes, which the
-// running softmax needs anyway, tells whether a chunk holds anything.
+// what is above it in LDS; the maximum of each lane's step, which the running
+// softmax needs anyway, tells whether a step holds anything.
 #include "common.h"
 #include "operators.h"
 
@@ -113,17 +113,15 @@ struct WaveBest {
     }
     if (t > lo) bar = (static_cast<u64>(t) << 32) - 1;   // every number of a logit at or above t is above it
   }
-  __device__ __forceinline__ void offer(u64 key, bool there, int lane) {
-    const u64 vote = __ballot(there && key > bar);
-    if (vote == 0) return;
+  // The least logit that can be above the bar.
+  __device__ __forceinline__ float floor() const { return key_logit(bar); }
+  // A number of every lane (0: none).
+  __device__ __forceinline__ void offer(u64 key, int lane) {
+    u64 vote = __ballot(key > bar);
     if (n + __popcll(vote) > kBufKeys) {
       sort(lane);
-      return offer_once(key, there, lane);
+      vote = __ballot(key > bar);
     }
-    push(key, vote, lane);
-  }
-  __device__ __forceinline__ void offer_once(u64 key, bool there, int lane) { push(key, __ballot(there && key > bar), lane); }
-  __device__ __forceinline__ void push(u64 key, u64 vote, int lane) {
     if (vote >> lane & 1) buf[n + __popcll(vote & ((1ull << lane) - 1))] = key;
     n += __popcll(vote);
   }
@@ -141,41 +139,57 @@ __device__ __forceinline__ float exp_neg(float d) {
   return __builtin_amdgcn_exp2f(fmaf(d, hi, d * lo));
 }
 
-// N consecutive logits of a lane (words word0 ...; none below zero are there).
-template <int N>
-__device__ __forceinline__ void take_chunk(const float* x, int word0, bool there, WaveBest& best, LaneSum& ls, int lane) {
-  float top = -INFINITY;
+// One step of a lane: NV vectors of E logits, whose words start at word0 and lie
+// `apart` apart (those that do not exist: -inf).  A NaN or +inf makes the sum NaN,
+// which is seen afterwards: then those logits are left out and the step is
+// repeated, so that the usual step pays nothing for them.
+template <int NV, int E>
+__device__ __forceinline__ void take_step(float* x, int word0, int apart, WaveBest& best, LaneSum& ls, int& bad, int lane) {
+  float top, sum, m;
+  auto reduce = [&]() {
+    top = x[0];
 #pragma unroll
-  for (int e = 0; e < N; ++e) top = fmaxf(top, x[e]);
-  const float m = fmaxf(ls.max, top);
+    for (int i = 1; i < NV * E; ++i) top = fmaxf(top, x[i]);
+    m = fmaxf(ls.max, top);
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV * E; ++i) sum += exp_neg(x[i] - m);
+  };
+  reduce();
+  if (!(sum < INFINITY)) {             // something is not finite, or nothing is there yet (-inf - -inf)
+#pragma unroll
+    for (int i = 0; i < NV * E; ++i) x[i] = usable(x[i], bad);
+    reduce();
+  }
   if (m > -INFINITY) {
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < N; ++e) sum += exp_neg(x[e] - m);
-    const float f = exp_neg(ls.max - m);
-    ls.sum = fma(ls.sum, static_cast<double>(f), static_cast<double>(sum));
+    ls.sum = fma(ls.sum, static_cast<double>(exp_neg(ls.max - m)), static_cast<double>(sum));
     ls.max = m;
   }
-  const uint32_t top_bits = there ? float_key(top) : 0u;
-  if (__ballot(top_bits >= static_cast<uint32_t>(best.bar >> 32)) == 0) return;
+  const uint32_t top_bits = float_key(top + 0.f);
+  if (__ballot(top_bits > static_cast<uint32_t>(best.bar >> 32)) == 0 &&
+      __ballot(top_bits == static_cast<uint32_t>(best.bar >> 32)) == 0)
+    return;
   best.raise(top_bits);
 #pragma unroll
-  for (int e = 0; e < N; ++e) best.offer(key_of(x[e], word0 + e), there, lane);
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float y = x[v * E + e] + 0.f;
+      if (__ballot(y >= best.floor()) != 0) best.offer(key_of(y, word0 + v * apart + e), lane);
+    }
 }
 
 // Parts of a row: vectors of 16 bytes from the row's first aligned one on.
 // kVecs of them a lane and step, all requested before the first is used.
 constexpr int kVecs = 4;
 
+// Part `unit % parts` of row `unit / parts`, by one wave; buf: its list in LDS.
 template <typename T>
-__global__ __launch_bounds__(kRowWaves * kWave) void k_select_rows(SelectArgs a, SelectWs w, int parts, int steps) {
+__device__ __forceinline__ void row_part(const SelectArgs& a, const SelectWs& w, int parts, int steps, int unit, u64* buf,
+                                         int lane) {
   constexpr int E = Vec16<T>::N;
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const int unit = blockIdx.x * kRowWaves + wave;
-  if (unit >= a.B * a.beam * parts) return;
   const int row = unit / parts, part = unit - row * parts;
   if (!row_live(a, row)) return;
-  __shared__ u64 s_buf[kRowWaves][kBufKeys];
   const T* x = static_cast<const T*>(a.logits) + static_cast<size_t>(row) * a.ld;
   const int V = a.vocab;
   const int off = static_cast<int>(reinterpret_cast<uintptr_t>(x) / sizeof(T) % E);
@@ -184,7 +198,7 @@ __global__ __launch_bounds__(kRowWaves * kWave) void k_select_rows(SelectArgs a,
   const T* body = x + head;
 
   WaveBest best;
-  best.init(s_buf[wave], a.beam);
+  best.init(buf, a.beam);
   LaneSum ls{-INFINITY, 0.0};
   int bad = 0;
   const int v0 = part * steps * (kVecs * kWave);
@@ -200,31 +214,30 @@ __global__ __launch_bounds__(kRowWaves * kWave) void k_select_rows(SelectArgs a,
     for (int v = v0; v < v1; v += kVecs * kWave) {
       uint4 next[kVecs];
       load(min(v + kVecs * kWave, v1 - 1), next);
+      float f[kVecs * E];
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) {
-        const int at = v + i * kWave + lane;
-        float f[E];
         const uint32_t u[4] = {cur[i].x, cur[i].y, cur[i].z, cur[i].w};
-        const bool there = at < v1;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float r = sizeof(T) == 4 ? __uint_as_float(u[e & 3])
-                                         : __uint_as_float(e & 1 ? u[e / 2 & 3] & 0xffff0000u : u[e / 2 & 3] << 16);
-          const float y = usable(r, bad);
-          f[e] = there ? y : -INFINITY;
-        }
-        take_chunk<E>(f, head + at * E, there, best, ls, lane);
+        for (int e = 0; e < E; ++e)
+          f[i * E + e] = sizeof(T) == 4 ? __uint_as_float(u[e & 3])
+                                        : __uint_as_float(e & 1 ? u[e / 2 & 3] & 0xffff0000u : u[e / 2 & 3] << 16);
       }
+      if (v + kVecs * kWave > v1) {
+#pragma unroll
+        for (int i = 0; i < kVecs * E; ++i) f[i] = v + i / E * kWave + lane < v1 ? f[i] : -INFINITY;
+      }
+      take_step<kVecs, E>(f, head + (v + lane) * E, kWave * E, best, ls, bad, lane);
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) cur[i] = next[i];
     }
   }
-  if (part == 0) {   // the words before the first aligned vector and behind the last
+  if (part == 0 && vecs * E < V) {   // the words before the first aligned vector and behind the last
     const int tail = head + vecs * E;
     const int word = lane < head ? lane : tail + (lane - head);
-    const bool there = word < V && (lane < head || lane - head < V - tail);
-    const float f = there ? usable(Elt<T>::load(x, word), bad) : -INFINITY;
-    take_chunk<1>(&f, word, there, best, ls, lane);
+    const bool there = lane < head || lane - head < V - tail;
+    float f = there ? Elt<T>::load(x, word) : -INFINITY;
+    take_step<1, 1>(&f, word, 0, best, ls, bad, lane);
   }
   best.sort(lane);
   const float m = wave_max(ls.max);
@@ -237,26 +250,71 @@ __global__ __launch_bounds__(kRowWaves * kWave) void k_select_rows(SelectArgs a,
   if (lane == 0) w.stat[out] = PartStat{s, m, any != 0 ? 1 : 0};
 }
 
-constexpr int kMergeWaves = 4;
-constexpr int kMergeThreads = kMergeWaves * kWave;
-
-__global__ __launch_bounds__(kMergeThreads) void k_select_merge(SelectArgs a, SelectWs w, int parts) {
-  const int b = blockIdx.x, K = a.beam;
+template <typename T>
+__global__ __launch_bounds__(kRowWaves * kWave) void k_select_rows(SelectArgs a, SelectWs w, int parts, int steps) {
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  __shared__ u64 s_buf[kMergeWaves][kBufKeys];
-  __shared__ u64 s_key[kMaxBeam][kMaxBeam];      // a beam's best numbers, best first (0: none; finished: one, the score)
-  __shared__ int s_n[kMaxBeam];                  // how many
-  __shared__ double s_lse[kMaxBeam];             // log-sum-exp
-  __shared__ double s_div[kMaxBeam];             // length^alpha
-  __shared__ int s_at[kMaxBeam];
-  __shared__ int s_bad;
-  if (threadIdx.x == 0) s_bad = 0;
-  if (threadIdx.x < K) s_at[threadIdx.x] = -1;
+  const int unit = blockIdx.x * kRowWaves + wave;
+  __shared__ u64 s_buf[kRowWaves][kBufKeys];
+  if (unit < a.B * a.beam * parts) row_part<T>(a, w, parts, steps, unit, s_buf[wave], lane);
+}
+
+// Largest of the wave's values.
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = max(v, dpp_u<kDppXor1>(v));
+  v = max(v, dpp_u<kDppXor2>(v));
+  v = max(v, dpp_u<kDppHalfMirror>(v));
+  v = max(v, dpp_u<kDppMirror>(v));
+  auto at = [&](int l) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), l)); };
+  return max(max(at(0), at(16)), max(at(32), at(48)));
+}
+// Order-preserving bits of a double (no NaN; -0 counts as 0).
+__device__ __forceinline__ u64 double_key(double d) {
+  const u64 u = static_cast<u64>(__double_as_longlong(d + 0.0));
+  return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+
+struct MergeLds {
+  u64 key[kMaxBeam][kMaxBeam];      // a beam's best numbers, best first
+  double lse[kMaxBeam], div[kMaxBeam];
+  float score[kMaxBeam];
+  int n[kMaxBeam];                  // a beam's candidates
+  int len[kMaxBeam];                // their length
+  int fin[kMaxBeam];
+  int at_beam[kMaxBeam], at_rank[kMaxBeam];
+  int bad;
+};
+
+// The survivors of sentence b, from its rows' part lists.  A wave per beam
+// merges the parts (it requests the statistics and the first kBatch x 64
+// numbers before it uses any); then the first wave merges the beams, a lane
+// each with its best candidate that is left, the largest key and of those the
+// lowest lane first.
+constexpr int kBatch = 6;
+
+template <int MW>
+__device__ __forceinline__ void merge_sentence(const SelectArgs& a, const SelectWs& w, int parts, int b, MergeLds& sm,
+                                               u64* buf, int lane, int wave) {
+  const int K = a.beam;
+  if (threadIdx.x == 0) sm.bad = 0;
   __syncthreads();
-  for (int k = wave; k < K; k += kMergeWaves) {  // a wave per beam
+  for (int k = wave; k < K; k += MW) {
     const int row = b * K + k;
     const float score = a.scores[row];
     const bool fin = a.done[row] != 0;
+    const int len = a.lens[row] + (fin ? 0 : 1);
+    const size_t p0 = static_cast<size_t>(row) * parts;
+    const int total = parts * K;
+    u64 key[kBatch];
+    auto load = [&](int i0) {
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int at = i0 + i * kWave + lane;
+        const u64 x = w.keys[p0 * K + min(at, total - 1)];
+        key[i] = at < total ? x : 0;
+      }
+    };
+    load(0);
+    PartStat mine = w.stat[p0 + min(lane, parts - 1)];
     int n = 0;
     double lse = 0.0;
     if (!isfinite(score)) {
@@ -264,93 +322,112 @@ __global__ __launch_bounds__(kMergeThreads) void k_select_merge(SelectArgs a, Se
     } else if (fin) {
       n = 1;
     } else {
-      const size_t p0 = static_cast<size_t>(row) * parts;
-      float m = -INFINITY;
-      int bad = 0;
-      for (int p = lane; p < parts; p += kWave) {
-        m = fmaxf(m, w.stat[p0 + p].max);
-        bad |= w.stat[p0 + p].bad;
-      }
-      m = wave_max(m);
-      double s = 0.0;
-      for (int p = lane; p < parts; p += kWave) {
+      if (lane >= parts) mine = PartStat{0.0, -INFINITY, 0};
+      for (int p = lane + kWave; p < parts; p += kWave) {
         const PartStat st = w.stat[p0 + p];
-        if (st.max > -INFINITY) s += st.sum * exp(static_cast<double>(st.max) - static_cast<double>(m));
+        const float m = fmaxf(mine.max, st.max);
+        if (m > -INFINITY)
+          mine.sum = mine.sum * exp(static_cast<double>(mine.max) - static_cast<double>(m)) +
+                     st.sum * exp(static_cast<double>(st.max) - static_cast<double>(m));
+        mine.max = m;
+        mine.bad |= st.bad;
       }
+      const float m = wave_max(mine.max);
+      double s = mine.max > -INFINITY ? mine.sum * exp(static_cast<double>(mine.max) - static_cast<double>(m)) : 0.0;
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
       lse = static_cast<double>(m) + log(s);
-      if (__ballot(bad != 0) != 0 && lane == 0) s_bad = 1;
+      if (__ballot(mine.bad != 0) != 0 && lane == 0) sm.bad = 1;
       WaveBest best;
-      best.init(s_buf[wave], K);
-      for (int i0 = 0; i0 < parts * K; i0 += kWave) {
-        const int i = i0 + lane;
-        const u64 key = i < parts * K ? w.keys[p0 * K + i] : 0;
-        if (__ballot(key > best.bar) == 0) continue;
-        best.raise(static_cast<uint32_t>(key >> 32));
-        best.offer(key, key != 0, lane);
+      best.init(buf, K);
+      for (int i0 = 0; i0 < total; i0 += kBatch * kWave) {
+        if (i0 > 0) load(i0);
+        u64 top = key[0];
+#pragma unroll
+        for (int i = 1; i < kBatch; ++i) top = key[i] > top ? key[i] : top;
+        if (__ballot(top > best.bar) == 0) continue;
+        best.raise(static_cast<uint32_t>(top >> 32));
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+          if (__ballot(key[i] > best.bar) != 0) best.offer(key[i], lane);
       }
       best.sort(lane);
       n = best.n;
-      for (int i = lane; i < n; i += kWave) s_key[k][i] = best.buf[i];
+      for (int i = lane; i < n; i += kWave) sm.key[k][i] = best.buf[i];
     }
     if (lane == 0) {
-      const int len = a.lens[row] + (fin ? 0 : 1);
-      s_n[k] = n;
-      s_lse[k] = lse;
-      s_div[k] = pow(static_cast<double>(len > 1 ? len : 1), static_cast<double>(a.alpha));
+      sm.n[k] = n;
+      sm.lse[k] = lse;
+      sm.div[k] = pow(static_cast<double>(len > 1 ? len : 1), static_cast<double>(a.alpha));
+      sm.score[k] = score;
+      sm.len[k] = len;
+      sm.fin[k] = fin ? 1 : 0;
     }
   }
   __syncthreads();
   auto cum_of = [&](int k, int r) -> double {
-    const int row = b * K + k;
-    const double score = a.scores[row];
-    return a.done[row] != 0 ? score : score + (static_cast<double>(key_logit(s_key[k][r])) - s_lse[k]);
+    const double score = sm.score[k];
+    return sm.fin[k] ? score : score + (static_cast<double>(key_logit(sm.key[k][r])) - sm.lse[k]);
   };
-  // every candidate counts those before it: (key, beam, rank in the beam).  A
-  // beam's candidates are in order, so those of another beam are found by halving.
-  for (int c = threadIdx.x; c < K * K; c += kMergeThreads) {
-    const int r = c / K, k = c - r * K;
-    if (r >= s_n[k]) continue;
-    const double key = cum_of(k, r) / s_div[k];
-    int rank = r;
-    for (int o = 0; o < K && rank < K; ++o) {
-      if (o == k) continue;
-      int lo = 0, hi = s_n[o];           // the first of beam o that comes after the candidate
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        const double other = cum_of(o, mid) / s_div[o];
-        if (other > key || (other == key && o < k)) lo = mid + 1;
-        else hi = mid;
+  if (wave == 0) {
+    const int k = lane < K ? lane : 0;
+    int r = 0;
+    u64 head = lane < K && sm.n[k] > 0 ? double_key(cum_of(k, 0) / sm.div[k]) : 0;
+    for (int j = 0; j < K; ++j) {
+      const uint32_t hi = static_cast<uint32_t>(head >> 32), hi_max = wave_max_u32(hi);
+      u64 vote = __ballot(hi == hi_max);
+      if (__popcll(vote) > 1) {
+        const uint32_t lo = hi == hi_max ? static_cast<uint32_t>(head) : 0u, lo_max = wave_max_u32(lo);
+        vote = __ballot(hi == hi_max && lo == lo_max);
       }
-      rank += lo;
+      const int win = __ffsll(static_cast<long long>(vote)) - 1;
+      if (lane == win) {
+        sm.at_beam[j] = head == 0 ? -1 : lane;
+        sm.at_rank[j] = r;
+        ++r;
+        head = head != 0 && r < sm.n[k] ? double_key(cum_of(k, r) / sm.div[k]) : 0;
+      }
     }
-    if (rank < K) s_at[rank] = c;
   }
-  __syncthreads();
-  float o_score = -INFINITY;
-  int o_par = -1, o_tok = a.pad_id, o_len = 0, o_done = 1;
+  __syncthreads();   // the outputs may be the inputs' own arrays: everything has been read
   const int t = threadIdx.x;
-  if (t < K && s_at[t] >= 0) {
-    const int c = s_at[t], r = c / K, k = c - r * K, row = b * K + k;
-    const bool fin = a.done[row] != 0;
-    o_score = static_cast<float>(cum_of(k, r));
-    o_par = k;
-    o_tok = fin ? a.pad_id : key_word(s_key[k][r]);
-    o_len = a.lens[row] + (fin ? 0 : 1);
-    o_done = fin || o_tok == a.eos_id || (a.max_len != nullptr && o_len >= a.max_len[b]) ? 1 : 0;
-  }
-  __syncthreads();   // the outputs may be the inputs' own arrays
   if (t < K) {
-    const int o = b * K + t;
-    a.out_scores[o] = o_score;
-    a.out_parent[o] = o_par;
-    a.out_token[o] = o_tok;
-    a.out_len[o] = o_len;
-    a.out_done[o] = o_done;
-    a.out_src[o] = o_done ? -1 : b * K + o_par;
+    const int k = sm.at_beam[t], r = sm.at_rank[t], o = b * K + t;
+    const bool there = k >= 0;
+    const bool fin = there && sm.fin[k] != 0;
+    const int tok = !there || fin ? a.pad_id : key_word(sm.key[k][r]);
+    const int len = there ? sm.len[k] : 0;
+    const int done = !there || fin || tok == a.eos_id || (a.max_len != nullptr && len >= a.max_len[b]) ? 1 : 0;
+    a.out_scores[o] = there ? static_cast<float>(cum_of(k, r)) : -INFINITY;
+    a.out_parent[o] = k;
+    a.out_token[o] = tok;
+    a.out_len[o] = len;
+    a.out_done[o] = done;
+    a.out_src[o] = done ? -1 : b * K + k;
   }
-  if (t == 0) a.out_flags[b] = s_bad ? 8 : 0;
+  if (t == 0) a.out_flags[b] = sm.bad ? 8 : 0;
+}
+
+template <int MW>
+__global__ __launch_bounds__(MW * kWave) void k_select_merge(SelectArgs a, SelectWs w, int parts) {
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  __shared__ u64 s_buf[MW][kBufKeys];
+  __shared__ MergeLds sm;
+  merge_sentence<MW>(a, w, parts, blockIdx.x, sm, s_buf[wave], lane, wave);
+}
+
+// Both stages of a sentence whose parts are at most as many as a workgroup's waves.
+constexpr int kSmallWaves = 16;
+
+template <typename T>
+__global__ __launch_bounds__(kSmallWaves * kWave) void k_select_small(SelectArgs a, SelectWs w, int parts, int steps) {
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  __shared__ u64 s_buf[kSmallWaves][kBufKeys];
+  __shared__ MergeLds sm;
+  if (wave < a.beam * parts) row_part<T>(a, w, parts, steps, blockIdx.x * a.beam * parts + wave, s_buf[wave], lane);
+  __threadfence_block();
+  __syncthreads();
+  merge_sentence<kSmallWaves>(a, w, parts, blockIdx.x, sm, s_buf[wave], lane, wave);
 }
 
 // Parts of a row and the steps of a part: kWantWaves waves in all where the
@@ -385,12 +462,20 @@ hipError_t launch_beam_select(const SelectArgs& a, hipStream_t s) {
   SelectWs w;
   w.stat = reinterpret_cast<PartStat*>(a.ws);
   w.keys = reinterpret_cast<u64*>(w.stat + units);
+  if (a.beam * sp.parts <= kSmallWaves) {
+    const dim3 grid(a.B), block(kSmallWaves * kWave);
+    if (a.dtype == DT_BF16) hipLaunchKernelGGL(k_select_small<bf16_t>, grid, block, 0, s, a, w, sp.parts, sp.steps);
+    else hipLaunchKernelGGL(k_select_small<float>, grid, block, 0, s, a, w, sp.parts, sp.steps);
+    return hipGetLastError();
+  }
   const dim3 grid(static_cast<unsigned>((units + kRowWaves - 1) / kRowWaves)), block(kRowWaves * kWave);
   if (a.dtype == DT_BF16) hipLaunchKernelGGL(k_select_rows<bf16_t>, grid, block, 0, s, a, w, sp.parts, sp.steps);
   else hipLaunchKernelGGL(k_select_rows<float>, grid, block, 0, s, a, w, sp.parts, sp.steps);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_select_merge, dim3(a.B), dim3(kMergeThreads), 0, s, a, w, sp.parts);
+  if (a.beam <= 4) hipLaunchKernelGGL(k_select_merge<4>, dim3(a.B), dim3(4 * kWave), 0, s, a, w, sp.parts);
+  else if (a.beam <= 8) hipLaunchKernelGGL(k_select_merge<8>, dim3(a.B), dim3(8 * kWave), 0, s, a, w, sp.parts);
+  else hipLaunchKernelGGL(k_select_merge<16>, dim3(a.B), dim3(16 * kWave), 0, s, a, w, sp.parts);
   return hipGetLastError();
 }
 

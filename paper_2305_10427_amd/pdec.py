@@ -416,9 +416,20 @@ def _scope(dev, stream):
     return contextlib.nullcontext()
 
 
+def _raw_stream(dev) -> int:
+    """Handle of the current stream of dev (torch.cuda.current_stream(dev).cuda_stream without making a Stream)."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(dev.index)
+
+
 def _tensor(name, t, dtypes, shape, dev, contiguous=True):
     """Refuses anything but a tensor of one of the dtypes, of the shape (None: any size) on the device."""
     import torch
+    try:                                     # the usual case, quickly
+        if t.dtype in dtypes and t.shape == shape and t.device == dev and t.is_cuda and (not contiguous or t.is_contiguous()):
+            return t
+    except AttributeError:
+        pass
     if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
         raise PdError(1, f"{name} must be a tensor of {' or '.join(str(d) for d in dtypes)}")
     if t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
@@ -462,13 +473,13 @@ def beam_select(logits, scores, lens, done, *, eos_id: int = C.EOS_ID, pad_id: i
     with _scope(dev, stream):
         out = torch.empty_like(scores)
         ints = torch.empty((5, B, K), dtype=torch.int32, device=dev)
-        flags = torch.empty(B, dtype=torch.int32, device=dev)
-        ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
+        flags = torch.empty((B,), dtype=torch.int32, device=dev)
+        ws = torch.empty((n.value,), dtype=torch.uint8, device=dev)
         at, step = ints.data_ptr(), 4 * B * K
         _check(L.pd_beam_select(logits.data_ptr(), dt, ld, B, K, V, scores.data_ptr(), lens.data_ptr(),
                                 done.data_ptr(), max_len.data_ptr() if max_len is not None else None, eos_id, pad_id,
                                 alpha, out.data_ptr(), at, at + step, at + 2 * step, at + 3 * step, at + 4 * step,
-                                flags.data_ptr(), ws.data_ptr(), n.value, _stream_handle(None)))
+                                flags.data_ptr(), ws.data_ptr(), n.value, _raw_stream(dev)))
     return BeamStep(out, *ints.unbind(0), flags)
 
 
@@ -558,7 +569,7 @@ class PagedCache:
                                      vp, ndt, nld, table.data_ptr(), ld, lens.data_ptr(), S, group, top,
                                      self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
                                      int(odt == torch.bfloat16), H * self.head_dim, ws.data_ptr() if n else None, n,
-                                     _stream_handle(None)))
+                                     _raw_stream(self.device)))
         return out
 
     def read(self, table, lens, first, *, layer: int = 0, count: int = 1, stream=None):
@@ -572,7 +583,7 @@ class PagedCache:
                     for _ in range(2))
             _check(load_library().pd_cache_read(self._p, layer, table.data_ptr(), ld, lens.data_ptr(), S,
                                                 first.data_ptr(), count, k.data_ptr(), v.data_ptr(),
-                                                _stream_handle(None)))
+                                                _raw_stream(self.device)))
         return k, v
 
     def fork(self, table, lens, parents, *, grow: bool = True, stream=None) -> PageFork:
@@ -590,7 +601,7 @@ class PagedCache:
             ws = torch.empty(n, dtype=torch.uint8, device=self.device)
             _check(load_library().pd_pages_fork(self._p, table.data_ptr(), ld, lens.data_ptr(), S, parents.data_ptr(),
                                                 n_out, int(grow), new.data_ptr(), out_lens.data_ptr(), refs.data_ptr(),
-                                                status.data_ptr(), ws.data_ptr(), n, _stream_handle(None)))
+                                                status.data_ptr(), ws.data_ptr(), n, _raw_stream(self.device)))
         return PageFork(new, out_lens, refs, status)
 
     def compact(self, table, lens, *, stream=None) -> PageMoves:
@@ -605,5 +616,5 @@ class PagedCache:
             ws = torch.empty(n, dtype=torch.uint8, device=self.device)
             _check(load_library().pd_pages_compact(self._p, table.data_ptr(), ld, lens.data_ptr(), S, new.data_ptr(),
                                                    remap.data_ptr(), status.data_ptr(), ws.data_ptr(), n,
-                                                   _stream_handle(None)))
+                                                   _raw_stream(self.device)))
         return PageMoves(new, remap, status)
