@@ -127,6 +127,25 @@ struct WaveBest {
   }
 };
 
+// Sum of the wave's values, in the order of wave_sum.
+template <int CTRL> __device__ __forceinline__ double dpp_d(double v) {
+  const u64 u = static_cast<u64>(__double_as_longlong(v));
+  const uint32_t lo = dpp_u<CTRL>(static_cast<uint32_t>(u)), hi = dpp_u<CTRL>(static_cast<uint32_t>(u >> 32));
+  return __longlong_as_double(static_cast<long long>(static_cast<u64>(hi) << 32 | lo));
+}
+__device__ __forceinline__ double wave_sum_d(double v) {
+  v += dpp_d<kDppXor1>(v);
+  v += dpp_d<kDppXor2>(v);
+  v += dpp_d<kDppHalfMirror>(v);
+  v += dpp_d<kDppMirror>(v);
+  auto at = [&](int l) {
+    const u64 u = static_cast<u64>(__double_as_longlong(v));
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(u), l), hi = __builtin_amdgcn_readlane(static_cast<int>(u >> 32), l);
+    return __longlong_as_double(static_cast<long long>(static_cast<u64>(hi) << 32 | lo));
+  };
+  return (at(0) + at(16)) + (at(32) + at(48));
+}
+
 // Running maximum and sum of exp(x - max) of a lane.
 struct LaneSum {
   float max;
@@ -139,12 +158,12 @@ __device__ __forceinline__ float exp_neg(float d) {
   return __builtin_amdgcn_exp2f(fmaf(d, hi, d * lo));
 }
 
-// One step of a lane: NV vectors of E logits, whose words start at word0 and lie
-// `apart` apart (those that do not exist: -inf).  A NaN or +inf makes the sum NaN,
+// One step of a lane: NV vectors of E logits of the row, whose words start at
+// word0 and lie `apart` apart (those that do not exist: -inf).  A NaN or +inf makes the sum NaN,
 // which is seen afterwards: then those logits are left out and the step is
 // repeated, so that the usual step pays nothing for them.
-template <int NV, int E>
-__device__ __forceinline__ void take_step(float* x, int word0, int apart, WaveBest& best, LaneSum& ls, int& bad, int lane) {
+template <typename T, int NV, int E>
+__device__ __forceinline__ void take_step(const T* row, float* x, int word0, int apart, WaveBest& best, LaneSum& ls, int& bad, int lane) {
   float top, sum, m;
   auto reduce = [&]() {
     top = x[0];
@@ -170,13 +189,22 @@ __device__ __forceinline__ void take_step(float* x, int word0, int apart, WaveBe
       __ballot(top_bits == static_cast<uint32_t>(best.bar >> 32)) == 0)
     return;
   best.raise(top_bits);
+  // which of the lane's logits are not below the bar; those few are read again
+  // rather than picked out of the registers, which would take all of them
+  // through the list's code one by one
+  const float floor = fmaxf(best.floor(), -3.4028235e38f);
+  uint32_t mask = 0;
 #pragma unroll
-  for (int v = 0; v < NV; ++v)
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float y = x[v * E + e] + 0.f;
-      if (__ballot(y >= best.floor()) != 0) best.offer(key_of(y, word0 + v * apart + e), lane);
+  for (int i = 0; i < NV * E; ++i) mask |= x[i] >= floor ? 1u << i : 0u;
+  while (__ballot(mask != 0) != 0) {
+    u64 key = 0;
+    if (mask != 0) {
+      const int i = __ffs(static_cast<int>(mask)) - 1, word = word0 + i / E * apart + i % E;
+      key = key_of(Elt<T>::load(row, word) + 0.f, word);
+      mask &= mask - 1;
     }
+    best.offer(key, lane);
+  }
 }
 
 // Parts of a row: vectors of 16 bytes from the row's first aligned one on.
@@ -227,7 +255,7 @@ __device__ __forceinline__ void row_part(const SelectArgs& a, const SelectWs& w,
 #pragma unroll
         for (int i = 0; i < kVecs * E; ++i) f[i] = v + i / E * kWave + lane < v1 ? f[i] : -INFINITY;
       }
-      take_step<kVecs, E>(f, head + (v + lane) * E, kWave * E, best, ls, bad, lane);
+      take_step<T, kVecs, E>(x, f, head + (v + lane) * E, kWave * E, best, ls, bad, lane);
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) cur[i] = next[i];
     }
@@ -237,13 +265,11 @@ __device__ __forceinline__ void row_part(const SelectArgs& a, const SelectWs& w,
     const int word = lane < head ? lane : tail + (lane - head);
     const bool there = lane < head || lane - head < V - tail;
     float f = there ? Elt<T>::load(x, word) : -INFINITY;
-    take_step<1, 1>(&f, word, 0, best, ls, bad, lane);
+    take_step<T, 1, 1>(x, &f, word, 0, best, ls, bad, lane);
   }
   best.sort(lane);
   const float m = wave_max(ls.max);
-  double s = ls.max > -INFINITY ? ls.sum * static_cast<double>(exp_neg(ls.max - m)) : 0.0;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  const double s = wave_sum_d(ls.max > -INFINITY ? ls.sum * static_cast<double>(exp_neg(ls.max - m)) : 0.0);
   const u64 any = __ballot(bad != 0);
   const size_t out = static_cast<size_t>(unit);
   for (int i = lane; i < a.beam; i += kWave) w.keys[out * a.beam + i] = i < best.n ? best.buf[i] : 0;
@@ -315,6 +341,9 @@ __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const Select
     };
     load(0);
     PartStat mine = w.stat[p0 + min(lane, parts - 1)];
+    double div = 1.0;                 // length^alpha, while the loads are under way
+    if (a.alpha == 1.f) div = static_cast<double>(max(len, 1));
+    else if (a.alpha != 0.f) div = pow(static_cast<double>(max(len, 1)), static_cast<double>(a.alpha));
     int n = 0;
     double lse = 0.0;
     if (!isfinite(score)) {
@@ -327,15 +356,12 @@ __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const Select
         const PartStat st = w.stat[p0 + p];
         const float m = fmaxf(mine.max, st.max);
         if (m > -INFINITY)
-          mine.sum = mine.sum * exp(static_cast<double>(mine.max) - static_cast<double>(m)) +
-                     st.sum * exp(static_cast<double>(st.max) - static_cast<double>(m));
+          mine.sum = mine.sum * static_cast<double>(exp_neg(mine.max - m)) + st.sum * static_cast<double>(exp_neg(st.max - m));
         mine.max = m;
         mine.bad |= st.bad;
       }
       const float m = wave_max(mine.max);
-      double s = mine.max > -INFINITY ? mine.sum * exp(static_cast<double>(mine.max) - static_cast<double>(m)) : 0.0;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+      const double s = wave_sum_d(mine.max > -INFINITY ? mine.sum * static_cast<double>(exp_neg(mine.max - m)) : 0.0);
       lse = static_cast<double>(m) + log(s);
       if (__ballot(mine.bad != 0) != 0 && lane == 0) sm.bad = 1;
       WaveBest best;
@@ -358,7 +384,7 @@ __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const Select
     if (lane == 0) {
       sm.n[k] = n;
       sm.lse[k] = lse;
-      sm.div[k] = pow(static_cast<double>(len > 1 ? len : 1), static_cast<double>(a.alpha));
+      sm.div[k] = div;
       sm.score[k] = score;
       sm.len[k] = len;
       sm.fin[k] = fin ? 1 : 0;
