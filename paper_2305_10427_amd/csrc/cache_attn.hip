@@ -6,6 +6,7 @@
 // j mod page_size of page table[s][j / page_size].  Keys of pages that do not
 // exist (an id outside the pool) are left out; a row without keys is zero.
 #include <type_traits>
+#include <utility>
 
 #include "common.h"
 #include "mma.h"
@@ -93,7 +94,7 @@ __device__ __forceinline__ uint32_t group_code(float x, float step, float least)
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kBlock = 32;                    // keys of an item
-constexpr int kListBlocks = 64;               // blocks whose items are listed at a time
+constexpr int kListBlocks = 32;               // blocks whose items are listed at a time
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Item {
@@ -138,14 +139,22 @@ __device__ __forceinline__ void take_off(float* v, uint4 p) {   // v -= p
 }
 
 // The eight codes of a word as bfloat16 16 + code: a code fills the top of the
-// mantissa of 16 (exact), two of them an instruction.  The offset and half the
-// code range are taken off inside the matrix product (kCodeMid), so that what
-// is accumulated is code - 7.5.
-__device__ __forceinline__ uint4 codes_bf16(uint32_t w) {
-  constexpr uint32_t m = 0x00780078u, e = 0x41804180u;
+// mantissa of 16 (exact), two of them in a shift and an AND-OR (whose masks are
+// kept in vector registers: the instruction takes no two constants).  The
+// offset is taken off inside the matrix product.  Scores take off 16; the
+// product with V takes off 16 + 7.5 and adds the middle of a group's range
+// apart, because its sum over many keys of differing sign would otherwise be a
+// small difference of large numbers.
+__device__ __forceinline__ uint4 codes_bf16(uint32_t w, uint32_t m, uint32_t e) {
   return make_uint4(((w << 3) & m) | e, ((w >> 1) & m) | e, ((w >> 5) & m) | e, ((w >> 9) & m) | e);
 }
+__device__ __forceinline__ uint32_t in_vgpr(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+constexpr uint32_t kCodeMask = 0x00780078u, kCodeExp = 0x41804180u;
 constexpr float kCodeMid = 7.5f;
+constexpr uint32_t kMinusOff2 = 0xc180c180u;   // two bfloat16 of -16
 constexpr uint32_t kMinusMid2 = 0xc1bcc1bcu;   // two bfloat16 of -(16 + 7.5)
 
 // The tokens at position len - 1 of the tile's beams, where that lies in keys
@@ -239,6 +248,75 @@ __device__ __forceinline__ void store_out(const AttendArgs& a, int s, int h, int
   }
 }
 
+// Lane L of every 16 lanes, to all of them (an operand modifier of the instruction that uses it).
+template <int L> __device__ __forceinline__ float row_lane(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x150 + L, 0xF, 0xF, true));
+}
+
+// The data of an item in registers: what lane (n, g) feeds the matrix cores, and
+// in 4 bits the (step, least) words of its row of lanes' eight keys, one lane
+// each (word w = key * groups + group in register w / 16 of lane w % 16).
+template <int CT, int DH> struct ItemData {
+  static constexpr int NU = DH >= 32 ? DH / 32 : 1;
+  static constexpr int NT = DH / 16;
+  static constexpr int NF = CT == CT_F32 ? DH / 16 : 1;
+  static constexpr int NW = NU >= 2 ? NU / 2 : 1;
+  uint32_t k4[2][CT == CT_INT4 ? NU : 1], v4[CT == CT_INT4 ? NT : 1], kp[CT == CT_INT4 ? NW : 1], vp[CT == CT_INT4 ? NW : 1];
+  uint4 kf[2][CT == CT_BF16 ? NU : 1], vf[CT == CT_BF16 ? NT : 1];
+  floatx4_t k32[2][NF], v32[CT == CT_F32 ? NT : 1][2];
+  // A page that is missing is never used: any block serves as its address.
+  __device__ __forceinline__ void load(const CacheView& c, int layer, int kv, const Item& it, int n, int g) {
+    const int ps = c.ps, j0 = it.block * kBlock;
+    const size_t hb0 = head_block(c, layer, max(it.id0, 0), kv), hb1 = head_block(c, layer, max(it.id1, 0), kv);
+    const size_t hb = g < 2 ? hb0 : hb1;                 // of keys 8 g ..
+    const int slot = (j0 + 8 * g) & (ps - 1);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int kappa = 8 * (n >> 2) + 4 * t + (n & 3);
+      const size_t row = (kappa < 16 ? hb0 : hb1) * ps + ((j0 + kappa) & (ps - 1));
+      if constexpr (CT == CT_F32) {
+        const float* p = reinterpret_cast<const float*>(c.k) + row * DH + 4 * g;
+#pragma unroll
+        for (int u = 0; u < NF; ++u) k32[t][u] = *reinterpret_cast<const floatx4_t*>(p + 16 * u);
+      } else if constexpr (CT == CT_BF16) {
+        const bf16_t* p = reinterpret_cast<const bf16_t*>(c.k) + row * DH + (DH >= 32 ? 8 * g : 8 * (g & 1));
+#pragma unroll
+        for (int u = 0; u < NU; ++u) kf[t][u] = *reinterpret_cast<const uint4*>(p + 32 * u);
+      } else {
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(c.k) + row * (DH / 8) + (DH >= 32 ? g : (g & 1));
+#pragma unroll
+        for (int u = 0; u < NU; ++u) k4[t][u] = p[4 * u];
+      }
+    }
+    if constexpr (CT == CT_INT4) {
+      const size_t at = (hb * ps + slot) * NU + (NU >= 2 ? n : n & 7);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        kp[w] = reinterpret_cast<const uint32_t*>(c.ks)[at + 16 * w];
+        vp[w] = reinterpret_cast<const uint32_t*>(c.vs)[at + 16 * w];
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const size_t at = (hb * DH + 16 * t + n) * ps + slot;
+      if constexpr (CT == CT_F32) {
+        v32[t][0] = *reinterpret_cast<const floatx4_t*>(reinterpret_cast<const float*>(c.v) + at);
+        v32[t][1] = *reinterpret_cast<const floatx4_t*>(reinterpret_cast<const float*>(c.v) + at + 4);
+      } else if constexpr (CT == CT_BF16) {
+        vf[t] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(c.v) + at);
+      } else {
+        v4[t] = reinterpret_cast<const uint32_t*>(c.v)[at >> 3];
+      }
+    }
+  }
+};
+
+// Calls f(integral_constant<int, 0>) ... f(integral_constant<int, N - 1>).
+template <typename F, int... I> __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F> __device__ __forceinline__ void each(F&& f) { each_of(std::make_integer_sequence<int, N>{}, f); }
+
 // Split of the launch: beams per tile, tiles of a group, ranges of the keys.
 struct Plan {
   int rows_per_tile, tiles, splits, blocks_per_split;
@@ -263,12 +341,19 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
   const int seq0 = grp * a.group + beam0;
   const int ps = c.ps;
 
-  __shared__ Item s_item[kListBlocks * 16];
-  __shared__ int4 s_tup[kListBlocks * 16];
+  // the lists and, once they are done, the waves' outputs share their LDS
+  struct Lists {
+    Item item[kListBlocks * 16];
+    int4 tup[kListBlocks * 16];
+  };
+  typedef float Outs[kWaves][16][DH + 4];
+  __shared__ __align__(16) char s_mem[sizeof(Lists) > sizeof(Outs) ? sizeof(Lists) : sizeof(Outs)];
+  Item* s_item = reinterpret_cast<Lists*>(s_mem)->item;
+  int4* s_tup = reinterpret_cast<Lists*>(s_mem)->tup;
+  Outs& s_o = *reinterpret_cast<Outs*>(s_mem);
   __shared__ int s_len[16];
   __shared__ int s_cnt[kWaves];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-  __shared__ float s_o[kWaves][16][DH + 4];
 
   if (threadIdx.x < 16)
     s_len[threadIdx.x] = static_cast<int>(threadIdx.x) < beams ? keys_of(a.lens, seq0 + threadIdx.x, a.max_len, a.table_ld, ps) : 0;
@@ -277,16 +362,16 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
   const bool row_ok = beam_n < beams;
   const size_t q0 = static_cast<size_t>(seq0 + (row_ok ? beam_n : 0)) * a.q_ld +
                     (static_cast<size_t>(kv) * G + (row_ok ? n % G : 0)) * DH;
-  const float s2 = a.scale * kLog2e;                  // scores in units of log 2
+  const float s2 = a.scale * kLog2e;                  // scores come out in units of log 2
   uint4 qf[CT == CT_F32 ? 1 : NU][3];
   floatx4_t q32[NF];
   float qsum[NU];                                     // 4 bits: sum of the row's queries over a group
-  floatx4_t qmid[NU];                                 // and -(16 + 7.5) times it
+  floatx4_t qoff[NU];                                 // and -16 times it
   if constexpr (CT == CT_F32) {
 #pragma unroll
     for (int u = 0; u < NF; ++u)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) q32[u][e] = row_ok ? load_any(a.q, a.q_bf16, q0 + 16 * u + 4 * g + e) : 0.f;
+      for (int e = 0; e < 4; ++e) q32[u][e] = row_ok ? s2 * load_any(a.q, a.q_bf16, q0 + 16 * u + 4 * g + e) : 0.f;
   } else {
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
@@ -294,7 +379,7 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const bool in = row_ok && (DH >= 32 || g < 2);
-        v[e] = in ? load_any(a.q, a.q_bf16, q0 + 32 * u + 8 * g + e) : 0.f;
+        v[e] = in ? s2 * load_any(a.q, a.q_bf16, q0 + 32 * u + 8 * g + e) : 0.f;
       }
       float sum = 0.f;
 #pragma unroll
@@ -306,10 +391,10 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
         take_off(v, qf[u][part]);
       }
       if constexpr (CT == CT_INT4) {
-        const uint4 mid = make_uint4(kMinusMid2, kMinusMid2, kMinusMid2, kMinusMid2);
-        qmid[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+        const uint4 off = make_uint4(kMinusOff2, kMinusOff2, kMinusOff2, kMinusOff2);
+        qoff[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int part = 0; part < 3; ++part) qmid[u] = mma_bf16(mid, qf[u][part], qmid[u]);
+        for (int part = 0; part < 3; ++part) qoff[u] = mma_bf16(off, qf[u][part], qoff[u]);
       }
     }
   }
@@ -323,6 +408,7 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
   // the step's own token, by the workgroup whose range holds its position
   if (a.new_k != nullptr) append_rows<CT, DH>(a, kv, seq0, beams, s_len, b_begin * kBlock, b_end * kBlock);
 
+  const uint32_t cm = CT == CT_INT4 ? in_vgpr(kCodeMask) : 0u, ce = CT == CT_INT4 ? in_vgpr(kCodeExp) : 0u;
   float m = -INFINITY, l = 0.f;
   floatx4_t acc[NT];
   float mid[NU];                                      // 4 bits: sum of p times the middle of a key's group, own keys
@@ -378,96 +464,56 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
       __syncthreads();
     }
 
+    // a wave's next item is requested before it works on the one it has
+    ItemData<CT, DH> cur, next;
+    Item it = s_item[wave < n_items ? wave : 0];
+    if (wave < n_items) cur.load(c, a.layer, kv, it, n, g);
     for (int i = wave; i < n_items; i += kWaves) {
-      const Item it = s_item[i];
+      const Item it_next = s_item[i + kWaves < n_items ? i + kWaves : i];
+      next.load(c, a.layer, kv, it_next, n, g);          // the last one once more at the end
       const int nv = it.rows_nv & 0xffff;
       const bool own = row_ok && ((it.rows_nv >> 16) >> beam_n & 1u);
-      const int j0 = it.block * kBlock;
       const bool whole = nv == kBlock && it.id0 >= 0 && it.id1 >= 0;
-      // head blocks of the two halves (a missing page is never used: any block serves as its address)
-      const size_t hb0 = head_block(c, a.layer, max(it.id0, 0), kv), hb1 = head_block(c, a.layer, max(it.id1, 0), kv);
-      // --- loads ---
-      const size_t hb_v = g < 2 ? hb0 : hb1;            // of keys 8 g ..
-      const int slot_v = (j0 + 8 * g) & (ps - 1);
-      uint32_t k4[2][NU], v4[NT];
-      uint4 kf[2][CT == CT_BF16 ? NU : 1], vf[CT == CT_BF16 ? NT : 1];
-      floatx4_t k32[2][NF], v32[CT == CT_F32 ? NT : 1][2];
-      uint32_t kp[8][NU], vp[8][NU];                    // (step, least) of the lane's keys 8 g + j
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int kappa = 8 * (n >> 2) + 4 * t + (n & 3);
-        const size_t row = (kappa < 16 ? hb0 : hb1) * ps + ((j0 + kappa) & (ps - 1));
-        if constexpr (CT == CT_F32) {
-          const float* p = reinterpret_cast<const float*>(c.k) + row * DH + 4 * g;
-#pragma unroll
-          for (int u = 0; u < NF; ++u) k32[t][u] = *reinterpret_cast<const floatx4_t*>(p + 16 * u);
-        } else if constexpr (CT == CT_BF16) {
-          const bf16_t* p = reinterpret_cast<const bf16_t*>(c.k) + row * DH + (DH >= 32 ? 8 * g : 8 * (g & 1));
-#pragma unroll
-          for (int u = 0; u < NU; ++u) kf[t][u] = *reinterpret_cast<const uint4*>(p + 32 * u);
-        } else {
-          const uint32_t* p = reinterpret_cast<const uint32_t*>(c.k) + row * (DH / 8) + (DH >= 32 ? g : (g & 1));
-#pragma unroll
-          for (int u = 0; u < NU; ++u) k4[t][u] = p[4 * u];
-        }
-      }
-      if constexpr (CT == CT_INT4) {
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(c.ks) + (hb_v * ps + slot_v) * NU;
-        const uint32_t* pv = reinterpret_cast<const uint32_t*>(c.vs) + (hb_v * ps + slot_v) * NU;
-#pragma unroll
-        for (int w = 0; w < 8 * NU; w += 4) {
-          const uint4 x = *reinterpret_cast<const uint4*>(p + w), y = *reinterpret_cast<const uint4*>(pv + w);
-          kp[w / NU][w % NU] = x.x; kp[(w + 1) / NU][(w + 1) % NU] = x.y;
-          kp[(w + 2) / NU][(w + 2) % NU] = x.z; kp[(w + 3) / NU][(w + 3) % NU] = x.w;
-          vp[w / NU][w % NU] = y.x; vp[(w + 1) / NU][(w + 1) % NU] = y.y;
-          vp[(w + 2) / NU][(w + 2) % NU] = y.z; vp[(w + 3) / NU][(w + 3) % NU] = y.w;
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const size_t at = (hb_v * DH + 16 * t + n) * ps + slot_v;
-        if constexpr (CT == CT_F32) {
-          v32[t][0] = *reinterpret_cast<const floatx4_t*>(reinterpret_cast<const float*>(c.v) + at);
-          v32[t][1] = *reinterpret_cast<const floatx4_t*>(reinterpret_cast<const float*>(c.v) + at + 4);
-        } else if constexpr (CT == CT_BF16) {
-          vf[t] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(c.v) + at);
-        } else {
-          v4[t] = reinterpret_cast<const uint32_t*>(c.v)[at >> 3];
-        }
-      }
       // --- scores of keys 8 g + j, in units of log 2 ---
-      float sc[8];
+      constexpr int NW = ItemData<CT, DH>::NW;
+      float sc[8], kstep[NW], kleast[NW];
+      if constexpr (CT == CT_INT4) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+        for (int w = 0; w < NW; ++w) {
+          kstep[w] = __uint_as_float(cur.kp[w] << 16);
+          kleast[w] = __uint_as_float(cur.kp[w] & 0xffff0000u);
+        }
+      }
+      each<2>([&](auto t_) {
+        constexpr int t = decltype(t_)::value;
         floatx4_t d = {0.f, 0.f, 0.f, 0.f};
         if constexpr (CT == CT_F32) {
 #pragma unroll
           for (int u = 0; u < NF; ++u)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d = mma_f32(k32[t][u][e], q32[u][e], d);
+            for (int e = 0; e < 4; ++e) d = mma_f32(cur.k32[t][u][e], q32[u][e], d);
         } else if constexpr (CT == CT_BF16) {
 #pragma unroll
           for (int u = 0; u < NU; ++u)
 #pragma unroll
-            for (int part = 0; part < 3; ++part) d = mma_bf16(kf[t][u], qf[u][part], d);
+            for (int part = 0; part < 3; ++part) d = mma_bf16(cur.kf[t][u], qf[u][part], d);
         } else {
-#pragma unroll
-          for (int u = 0; u < NU; ++u) {
-            floatx4_t x = qmid[u];
-            const uint4 w = codes_bf16(k4[t][u]);
+          each<NU>([&](auto u_) {
+            constexpr int u = decltype(u_)::value;
+            floatx4_t x = qoff[u];
+            const uint4 w = codes_bf16(cur.k4[t][u], cm, ce);
 #pragma unroll
             for (int part = 0; part < 3; ++part) x = mma_bf16(w, qf[u][part], x);
-#pragma unroll
-            for (int i2 = 0; i2 < 4; ++i2) {
-              const uint32_t pr = kp[4 * t + i2][u];
-              const float step = __uint_as_float(pr << 16), least = __uint_as_float(pr & 0xffff0000u);
-              d[i2] = fmaf(fmaf(kCodeMid, step, least), qsum[u], fmaf(step, x[i2], d[i2]));
-            }
-          }
+            each<4>([&](auto i_) {
+              constexpr int i2 = decltype(i_)::value, at = (4 * t + i2) * NU + u;
+              d[i2] = fmaf(row_lane<at % 16>(kstep[at / 16]), x[i2], d[i2]);
+              d[i2] = fmaf(row_lane<at % 16>(kleast[at / 16]), qsum[u], d[i2]);
+            });
+          });
         }
 #pragma unroll
-        for (int i2 = 0; i2 < 4; ++i2) sc[4 * t + i2] = d[i2] * s2;
-      }
+        for (int i2 = 0; i2 < 4; ++i2) sc[4 * t + i2] = d[i2];
+      });
       uint32_t live = 0xff;                             // keys of this lane that exist
       if (!whole) {
         const int here = (g < 2 ? it.id0 : it.id1) >= 0 ? max(0, min(8, nv - 8 * g)) : 0;
@@ -483,7 +529,7 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
       float p[8], sum = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        p[j] = (live >> j & 1u) ? __builtin_amdgcn_exp2f(sc[j] - mn) : 0.f;
+        p[j] = __builtin_amdgcn_exp2f(sc[j] - mn);         // 0 for a key that does not exist
         sum += p[j];
       }
       // --- weights times V ---
@@ -494,13 +540,13 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v32[t][j >> 2][j & 3] = (live >> j & 1u) ? v32[t][j >> 2][j & 3] : 0.f;
+            for (int j = 0; j < 8; ++j) cur.v32[t][j >> 2][j & 3] = (live >> j & 1u) ? cur.v32[t][j >> 2][j & 3] : 0.f;
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           o[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int j = 0; j < 8; ++j) o[t] = mma_f32(v32[t][j >> 2][j & 3], p[j], o[t]);
+          for (int j = 0; j < 8; ++j) o[t] = mma_f32(cur.v32[t][j >> 2][j & 3], p[j], o[t]);
         }
       } else if constexpr (CT == CT_BF16) {
         if (!whole) {
@@ -509,7 +555,8 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
           for (int j = 0; j < 4; ++j)
             mk[j] = ((live >> (2 * j) & 1u) ? 0xffffu : 0u) | ((live >> (2 * j + 1) & 1u) ? 0xffff0000u : 0u);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) vf[t] = make_uint4(vf[t].x & mk[0], vf[t].y & mk[1], vf[t].z & mk[2], vf[t].w & mk[3]);
+          for (int t = 0; t < NT; ++t)
+            cur.vf[t] = make_uint4(cur.vf[t].x & mk[0], cur.vf[t].y & mk[1], cur.vf[t].z & mk[2], cur.vf[t].w & mk[3]);
         }
         const uint4 hi = pack8(p);
         float r[8];
@@ -519,22 +566,30 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
         const uint4 lo = pack8(r);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          o[t] = mma_bf16(vf[t], hi, floatx4_t{0.f, 0.f, 0.f, 0.f});
-          o[t] = mma_bf16(vf[t], lo, o[t]);
+          o[t] = mma_bf16(cur.vf[t], hi, floatx4_t{0.f, 0.f, 0.f, 0.f});
+          o[t] = mma_bf16(cur.vf[t], lo, o[t]);
         }
       } else {
         const uint4 off = make_uint4(kMinusMid2, kMinusMid2, kMinusMid2, kMinusMid2);
+        float vstep[NW], vmid[NW];                        // a group's step and the middle of its range
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
+        for (int w = 0; w < NW; ++w) {
+          if (!whole) {                                   // what lies behind the sequence's end may be anything
+            const int key = (16 * w + (NU >= 2 ? n : n & 7)) / NU;
+            cur.vp[w] = (live >> key & 1u) ? cur.vp[w] : 0u;
+          }
+          vstep[w] = __uint_as_float(cur.vp[w] << 16);
+          vmid[w] = fmaf(kCodeMid, vstep[w], __uint_as_float(cur.vp[w] & 0xffff0000u));
+        }
+        each<NU>([&](auto u_) {
+          constexpr int u = decltype(u_)::value;
           float r[8];
           om[u] = 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const uint32_t pr = (whole || (live >> j & 1u)) ? vp[j][u] : 0u;
-            const float step = __uint_as_float(pr << 16), least = __uint_as_float(pr & 0xffff0000u);
-            r[j] = p[j] * step;
-            om[u] = fmaf(p[j], fmaf(kCodeMid, step, least), om[u]);
-          }
+          each<8>([&](auto j_) {
+            constexpr int j = decltype(j_)::value, at = j * NU + u;
+            r[j] = row_lane<at % 16>(vstep[at / 16]) * p[j];
+            om[u] = fmaf(row_lane<at % 16>(vmid[at / 16]), p[j], om[u]);
+          });
           const uint4 hi = pack8(r);
           take_off(r, hi);
           const uint4 lo = pack8(r);
@@ -542,11 +597,11 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
           base = mma_bf16(off, lo, base);
 #pragma unroll
           for (int t = u * (NT / NU); t < (u + 1) * (NT / NU); ++t) {
-            const uint4 w = codes_bf16(v4[t]);
+            const uint4 w = codes_bf16(cur.v4[t], cm, ce);
             o[t] = mma_bf16(w, hi, base);
             o[t] = mma_bf16(w, lo, o[t]);
           }
-        }
+        });
       }
       if (own) {
         l = fmaf(l, f, sum);
@@ -560,6 +615,8 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
           for (int u = 0; u < NU; ++u) mid[u] = fmaf(mid[u], f, om[u]);
         }
       }
+      cur = next;
+      it = it_next;
     }
   }
 
@@ -575,6 +632,7 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
         for (int e = 0; e < 4; ++e) acc[t][e] += x;
     }
   }
+  __syncthreads();                                    // every wave is done with the lists
   if (g == 0) {
     s_m[wave][n] = m;
     s_l[wave][n] = l;
@@ -611,30 +669,50 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
   }
 }
 
-// The parts of a row's key ranges, in their order: one lane per four dimensions.
+// The parts of a row's key ranges: a workgroup per row, DH / 4 lanes for each
+// kJoinThreads / (DH / 4)-th of the ranges, then those sums in order.
+constexpr int kJoinThreads = 256;
+
 template <int DH>
-__global__ __launch_bounds__(256) void k_join(AttendArgs a, int splits) {
-  const long long i = blockIdx.x * 256ll + threadIdx.x;
-  const int parts = a.n_seqs * a.heads;
-  const long long row = i / (DH / 4);
-  if (row >= parts) return;
-  const int d = 4 * static_cast<int>(i - row * (DH / 4));
+__global__ __launch_bounds__(kJoinThreads) void k_join(AttendArgs a, int splits) {
+  constexpr int L = DH / 4, Z = kJoinThreads / L;
+  const size_t row = blockIdx.x, parts = static_cast<size_t>(a.n_seqs) * a.heads;
+  const int dl = threadIdx.x % L, zl = threadIdx.x / L;
   const float* base = reinterpret_cast<const float*>(a.ws);
-  const float2* ml = reinterpret_cast<const float2*>(base + static_cast<size_t>(splits) * parts * DH);
+  const float2* ml = reinterpret_cast<const float2*>(base + splits * parts * DH);
+  __shared__ float s_m[kJoinThreads], s_l[Z];
+  __shared__ floatx4_t s_o[Z][L];
   float mt = -INFINITY;
-  for (int z = 0; z < splits; ++z) mt = fmaxf(mt, ml[static_cast<size_t>(z) * parts + row].x);
+  for (int z = threadIdx.x; z < splits; z += kJoinThreads) mt = fmaxf(mt, ml[z * parts + row].x);
+  mt = wave_max(mt);
+  if ((threadIdx.x & (kWave - 1)) == 0) s_m[threadIdx.x / kWave] = mt;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kJoinThreads / kWave; ++w) mt = fmaxf(mt, s_m[w]);
   float lt = 0.f;
   floatx4_t o = {0.f, 0.f, 0.f, 0.f};
-  for (int z = 0; z < splits; ++z) {
-    const size_t part = static_cast<size_t>(z) * parts + row;
-    const float2 x = ml[part];
+#pragma unroll 4
+  for (int z = zl; z < splits; z += Z) {
+    const float2 x = ml[z * parts + row];
+    const floatx4_t v = *reinterpret_cast<const floatx4_t*>(base + (z * parts + row) * DH + 4 * dl);
     const float f = x.x == -INFINITY && !(x.y != 0.f) ? 0.f : __builtin_amdgcn_exp2f(x.x - mt);
     lt = fmaf(x.y, f, lt);
-    const floatx4_t v = *reinterpret_cast<const floatx4_t*>(base + part * DH + d);
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], f, o[e]);
   }
-  store_out(a, static_cast<int>(row / a.heads), static_cast<int>(row % a.heads), d, o, lt);
+  s_o[zl][dl] = o;
+  if (dl == 0) s_l[zl] = lt;
+  __syncthreads();
+  if (zl == 0) {
+#pragma unroll 4
+    for (int i = 1; i < Z; ++i) {
+      lt += s_l[i];
+      const floatx4_t v = s_o[i][dl];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += v[e];
+    }
+    store_out(a, static_cast<int>(row / a.heads), static_cast<int>(row % a.heads), 4 * dl, o, lt);
+  }
 }
 
 __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
@@ -690,8 +768,7 @@ hipError_t launch_attend_t(const AttendArgs& a, const Plan& p, hipStream_t s) {
   hipLaunchKernelGGL((k_attend<CT, DH>), dim3(static_cast<unsigned>(wgs)), dim3(kThreads), 0, s, a, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  const long long lanes = static_cast<long long>(a.n_seqs) * a.heads * (DH / 4);
-  hipLaunchKernelGGL(k_join<DH>, dim3(static_cast<unsigned>((lanes + 255) / 256)), dim3(256), 0, s, a, p.splits);
+  hipLaunchKernelGGL(k_join<DH>, dim3(a.n_seqs * a.heads), dim3(kJoinThreads), 0, s, a, p.splits);
   return hipGetLastError();
 }
 
