@@ -253,63 +253,7 @@ template <int L> __device__ __forceinline__ float row_lane(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x150 + L, 0xF, 0xF, true));
 }
 
-// The data of an item in registers: what lane (n, g) feeds the matrix cores, and
-// in 4 bits the (step, least) words of its row of lanes' eight keys, one lane
-// each (word w = key * groups + group in register w / 16 of lane w % 16).
-template <int CT, int DH> struct ItemData {
-  static constexpr int NU = DH >= 32 ? DH / 32 : 1;
-  static constexpr int NT = DH / 16;
-  static constexpr int NF = CT == CT_F32 ? DH / 16 : 1;
-  static constexpr int NW = NU >= 2 ? NU / 2 : 1;
-  uint32_t k4[2][CT == CT_INT4 ? NU : 1], v4[CT == CT_INT4 ? NT : 1], kp[CT == CT_INT4 ? NW : 1], vp[CT == CT_INT4 ? NW : 1];
-  uint4 kf[2][CT == CT_BF16 ? NU : 1], vf[CT == CT_BF16 ? NT : 1];
-  floatx4_t k32[2][NF], v32[CT == CT_F32 ? NT : 1][2];
-  // A page that is missing is never used: any block serves as its address.
-  __device__ __forceinline__ void load(const CacheView& c, int layer, int kv, const Item& it, int n, int g) {
-    const int ps = c.ps, j0 = it.block * kBlock;
-    const size_t hb0 = head_block(c, layer, max(it.id0, 0), kv), hb1 = head_block(c, layer, max(it.id1, 0), kv);
-    const size_t hb = g < 2 ? hb0 : hb1;                 // of keys 8 g ..
-    const int slot = (j0 + 8 * g) & (ps - 1);
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int kappa = 8 * (n >> 2) + 4 * t + (n & 3);
-      const size_t row = (kappa < 16 ? hb0 : hb1) * ps + ((j0 + kappa) & (ps - 1));
-      if constexpr (CT == CT_F32) {
-        const float* p = reinterpret_cast<const float*>(c.k) + row * DH + 4 * g;
-#pragma unroll
-        for (int u = 0; u < NF; ++u) k32[t][u] = *reinterpret_cast<const floatx4_t*>(p + 16 * u);
-      } else if constexpr (CT == CT_BF16) {
-        const bf16_t* p = reinterpret_cast<const bf16_t*>(c.k) + row * DH + (DH >= 32 ? 8 * g : 8 * (g & 1));
-#pragma unroll
-        for (int u = 0; u < NU; ++u) kf[t][u] = *reinterpret_cast<const uint4*>(p + 32 * u);
-      } else {
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(c.k) + row * (DH / 8) + (DH >= 32 ? g : (g & 1));
-#pragma unroll
-        for (int u = 0; u < NU; ++u) k4[t][u] = p[4 * u];
-      }
-    }
-    if constexpr (CT == CT_INT4) {
-      const size_t at = (hb * ps + slot) * NU + (NU >= 2 ? n : n & 7);
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        kp[w] = reinterpret_cast<const uint32_t*>(c.ks)[at + 16 * w];
-        vp[w] = reinterpret_cast<const uint32_t*>(c.vs)[at + 16 * w];
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const size_t at = (hb * DH + 16 * t + n) * ps + slot;
-      if constexpr (CT == CT_F32) {
-        v32[t][0] = *reinterpret_cast<const floatx4_t*>(reinterpret_cast<const float*>(c.v) + at);
-        v32[t][1] = *reinterpret_cast<const floatx4_t*>(reinterpret_cast<const float*>(c.v) + at + 4);
-      } else if constexpr (CT == CT_BF16) {
-        vf[t] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16_t*>(c.v) + at);
-      } else {
-        v4[t] = reinterpret_cast<const uint32_t*>(c.v)[at >> 3];
-      }
-    }
-  }
-};
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 
 // Calls f(integral_constant<int, 0>) ... f(integral_constant<int, N - 1>).
 template <typename F, int... I> __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f) {
@@ -317,13 +261,113 @@ template <typename F, int... I> __device__ __forceinline__ void each_of(std::int
 }
 template <int N, typename F> __device__ __forceinline__ void each(F&& f) { each_of(std::make_integer_sequence<int, N>{}, f); }
 
+// The data of an item on its way: pieces of 16 bytes (8 where a row or the half
+// of one is no longer) in the order in which they lie in memory, neighbouring
+// lanes on neighbouring pieces, then through LDS into the order of the matrix
+// cores.  A lane that loads its operands itself takes 16 bytes (4 bits: 4) from
+// a row of its own, which keeps the address unit busy for 64 rows an
+// instruction: 64 x 4 rows of 4,000 keys of 64, bfloat16 3.2 TB/s and 4 bits
+// 1.1 TB/s that way.
+//
+// LDS: K rows in the order of the score tiles (key 8 a + 4 t + b in row
+// 16 t + 4 a + b), V rows by dimension, both padded so that the 16 rows of a read
+// start in different banks.  In 4 bits the (step, least) words of a row of
+// lanes' eight keys stay in registers, one a lane (word w = key * groups + group
+// in register w / 16 of lane w % 16).
+template <int CT, int DH> struct Stage {
+  static constexpr int NU = DH >= 32 ? DH / 32 : 1;
+  static constexpr int NW = NU >= 2 ? NU / 2 : 1;
+  static constexpr int kRow = CT == CT_F32 ? 4 * DH : CT == CT_BF16 ? 2 * DH : DH / 2;      // bytes of a key
+  static constexpr int kSeg = CT == CT_F32 ? 128 : CT == CT_BF16 ? 64 : 16;                 // of 32 keys of a dimension
+  static constexpr int kPiece = CT == CT_INT4 ? 8 : 16;
+  static constexpr int kRowLds = kRow >= 32 ? kRow + 16 : kRow;
+  static constexpr int kSegLds = kSeg > 16 ? kSeg + 16 : kSeg;
+  static constexpr int kBytes = kBlock * kRowLds + DH * kSegLds;                            // of a wave
+  static constexpr int NK = (kBlock * kRow / kPiece + kWave - 1) / kWave;                   // pieces a lane
+  static constexpr int NV = (DH * kSeg / kPiece + kWave - 1) / kWave;
+  static constexpr int PK = kRow / kPiece, PH = kSeg / 2 / kPiece;                          // pieces of a key, of half a segment
+  static constexpr bool kFullK = kBlock * PK % kWave == 0, kFullV = DH * 2 * PH % kWave == 0;
+  typedef typename std::conditional<kPiece == 16, u32x4_t, u32x2_t>::type Piece;
+  Piece k[NK], v[NV];
+  uint32_t kp[CT == CT_INT4 ? NW : 1], vp[CT == CT_INT4 ? NW : 1];
+  // A page that is missing is never used: any block serves as its address.
+  __device__ __forceinline__ void load(const CacheView& c, int layer, int kv, const Item& it, int lane) {
+    const int ps = c.ps, j0 = it.block * kBlock;
+    const size_t hb0 = head_block(c, layer, max(it.id0, 0), kv), hb1 = head_block(c, layer, max(it.id1, 0), kv);
+    const int s0 = j0 & (ps - 1), s1 = (j0 + 16) & (ps - 1);      // slots of the halves
+    const char* k0 = c.k + (hb0 * ps + s0) * kRow;
+    const char* k1 = c.k + (hb1 * ps + s1) * kRow;
+    const int dim_bytes = ps * kSeg / kBlock;                     // from a dimension to the next
+    const char* v0 = c.v + hb0 * DH * dim_bytes + s0 * kSeg / kBlock;
+    const char* v1 = c.v + hb1 * DH * dim_bytes + s1 * kSeg / kBlock;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      int x = i * kWave + lane;
+      if (!kFullK) x = min(x, kBlock * PK - 1);
+      const bool up = x >= 16 * PK;
+      k[i] = *reinterpret_cast<const Piece*>((up ? k1 : k0) + (x - (up ? 16 * PK : 0)) * kPiece);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      int dim, half, q;
+      v_place(i, lane, ps, dim, half, q);
+      v[i] = *reinterpret_cast<const Piece*>((half ? v1 : v0) + dim * dim_bytes + q * kPiece);
+    }
+    if constexpr (CT == CT_INT4) {
+      const int n = lane & 15, g = lane >> 4;
+      const size_t at = ((g < 2 ? hb0 * ps + s0 : hb1 * ps + s1) + 8 * (g & 1)) * NU + (NU >= 2 ? n : n & 7);
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        kp[w] = reinterpret_cast<const uint32_t*>(c.ks)[at + 16 * w];
+        vp[w] = reinterpret_cast<const uint32_t*>(c.vs)[at + 16 * w];
+      }
+    }
+  }
+  // Piece i of a lane: pages of 16 keys are taken one after the other, longer
+  // ones a dimension at a time.
+  static __device__ __forceinline__ void v_place(int i, int lane, int ps, int& dim, int& half, int& q) {
+    int x = i * kWave + lane;
+    if (!kFullV) x = min(x, DH * 2 * PH - 1);
+    q = x % PH;
+    if (ps == 16) {
+      half = x >= DH * PH ? 1 : 0;
+      dim = x / PH - half * DH;
+    } else {
+      half = x / PH & 1;
+      dim = x / (2 * PH);
+    }
+  }
+  __device__ __forceinline__ void store(char* lds, int lane, int ps) const {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      int x = i * kWave + lane;
+      if (!kFullK) x = min(x, kBlock * PK - 1);
+      const int key = x / PK, row = (key & 4) * 4 + (key >> 3) * 4 + (key & 3);
+      *reinterpret_cast<Piece*>(lds + row * kRowLds + x % PK * kPiece) = k[i];
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      int dim, half, q;
+      v_place(i, lane, ps, dim, half, q);
+      *reinterpret_cast<Piece*>(lds + kBlock * kRowLds + dim * kSegLds + half * (kSeg / 2) + q * kPiece) = v[i];
+    }
+  }
+};
+
+template <int CT> constexpr int kSegLane = CT == CT_F32 ? 32 : CT == CT_BF16 ? 16 : 4;   // bytes of eight keys of a dimension
+
 // Split of the launch: beams per tile, tiles of a group, ranges of the keys.
 struct Plan {
   int rows_per_tile, tiles, splits, blocks_per_split;
 };
 
+// Waves a SIMD's registers are to hold.
+constexpr int waves_per_simd(int ct, int dh) {
+  return ct == CT_F32 ? (dh >= 128 ? 1 : dh == 64 ? 2 : 4) : dh >= 128 ? 2 : dh == 64 ? 3 : 4;
+}
+
 template <int CT, int DH>
-__global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
+__global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(AttendArgs a, Plan pl) {
   constexpr int NU = DH >= 32 ? DH / 32 : 1;          // steps of 32 dimensions (bf16 products), groups of a cache in 4 bits
   constexpr int NT = DH / 16;                         // tiles of 16 dimensions
   constexpr int NF = CT == CT_F32 ? DH / 16 : 1;      // float: steps of 16 dimensions
@@ -341,16 +385,23 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
   const int seq0 = grp * a.group + beam0;
   const int ps = c.ps;
 
-  // the lists and, once they are done, the waves' outputs share their LDS
+  // the lists, the items' data and at the end the waves' outputs share their LDS
+  typedef Stage<CT, DH> SG;
   struct Lists {
     Item item[kListBlocks * 16];
-    int4 tup[kListBlocks * 16];
+    union {
+      int4 tup[kListBlocks * 16];
+      char stage[kWaves][SG::kBytes];
+    };
   };
   typedef float Outs[kWaves][16][DH + 4];
   __shared__ __align__(16) char s_mem[sizeof(Lists) > sizeof(Outs) ? sizeof(Lists) : sizeof(Outs)];
   Item* s_item = reinterpret_cast<Lists*>(s_mem)->item;
   int4* s_tup = reinterpret_cast<Lists*>(s_mem)->tup;
   Outs& s_o = *reinterpret_cast<Outs*>(s_mem);
+  char* lds = reinterpret_cast<Lists*>(s_mem)->stage[wave];
+  const char* k_lds = lds + n * SG::kRowLds + (CT == CT_INT4 ? (DH >= 32 ? 4 * g : 4 * (g & 1)) : CT == CT_BF16 && DH < 32 ? 16 * (g & 1) : 16 * g);
+  const char* v_lds = lds + kBlock * SG::kRowLds + n * SG::kSegLds + kSegLane<CT> * g;
   __shared__ int s_len[16];
   __shared__ int s_cnt[kWaves];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
@@ -464,24 +515,31 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
       __syncthreads();
     }
 
-    // a wave's next item is requested before it works on the one it has
-    ItemData<CT, DH> cur, next;
-    Item it = s_item[wave < n_items ? wave : 0];
-    if (wave < n_items) cur.load(c, a.layer, kv, it, n, g);
+    // a wave's items: one in LDS, the next one on its way in registers
+    Stage<CT, DH> st;
+    uint32_t kp[SG::NW], vp[SG::NW];
+    if (wave < n_items) st.load(c, a.layer, kv, s_item[wave], lane);
     for (int i = wave; i < n_items; i += kWaves) {
-      const Item it_next = s_item[i + kWaves < n_items ? i + kWaves : i];
-      next.load(c, a.layer, kv, it_next, n, g);          // the last one once more at the end
+      const Item it = s_item[i];
+      wave_lds_sync();                                   // the wave is done with the item before
+      st.store(lds, lane, ps);
+#pragma unroll
+      for (int w = 0; w < SG::NW; ++w) {
+        if constexpr (CT == CT_INT4) kp[w] = st.kp[w], vp[w] = st.vp[w];
+      }
+      wave_lds_sync();
+      if (i + kWaves < n_items) st.load(c, a.layer, kv, s_item[i + kWaves], lane);
       const int nv = it.rows_nv & 0xffff;
       const bool own = row_ok && ((it.rows_nv >> 16) >> beam_n & 1u);
       const bool whole = nv == kBlock && it.id0 >= 0 && it.id1 >= 0;
       // --- scores of keys 8 g + j, in units of log 2 ---
-      constexpr int NW = ItemData<CT, DH>::NW;
+      constexpr int NW = SG::NW;
       float sc[8], kstep[NW], kleast[NW];
       if constexpr (CT == CT_INT4) {
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-          kstep[w] = __uint_as_float(cur.kp[w] << 16);
-          kleast[w] = __uint_as_float(cur.kp[w] & 0xffff0000u);
+          kstep[w] = __uint_as_float(kp[w] << 16);
+          kleast[w] = __uint_as_float(kp[w] & 0xffff0000u);
         }
       }
       each<2>([&](auto t_) {
@@ -489,19 +547,23 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
         floatx4_t d = {0.f, 0.f, 0.f, 0.f};
         if constexpr (CT == CT_F32) {
 #pragma unroll
-          for (int u = 0; u < NF; ++u)
+          for (int u = 0; u < NF; ++u) {
+            const floatx4_t x = *reinterpret_cast<const floatx4_t*>(k_lds + t * 16 * SG::kRowLds + 64 * u);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d = mma_f32(cur.k32[t][u][e], q32[u][e], d);
+            for (int e = 0; e < 4; ++e) d = mma_f32(x[e], q32[u][e], d);
+          }
         } else if constexpr (CT == CT_BF16) {
 #pragma unroll
-          for (int u = 0; u < NU; ++u)
+          for (int u = 0; u < NU; ++u) {
+            const uint4 x = *reinterpret_cast<const uint4*>(k_lds + t * 16 * SG::kRowLds + 64 * u);
 #pragma unroll
-            for (int part = 0; part < 3; ++part) d = mma_bf16(cur.kf[t][u], qf[u][part], d);
+            for (int part = 0; part < 3; ++part) d = mma_bf16(x, qf[u][part], d);
+          }
         } else {
           each<NU>([&](auto u_) {
             constexpr int u = decltype(u_)::value;
             floatx4_t x = qoff[u];
-            const uint4 w = codes_bf16(cur.k4[t][u], cm, ce);
+            const uint4 w = codes_bf16(*reinterpret_cast<const uint32_t*>(k_lds + t * 16 * SG::kRowLds + 16 * u), cm, ce);
 #pragma unroll
             for (int part = 0; part < 3; ++part) x = mma_bf16(w, qf[u][part], x);
             each<4>([&](auto i_) {
@@ -536,27 +598,24 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
       floatx4_t o[NT];
       float om[NU];
       if constexpr (CT == CT_F32) {
-        if (!whole) {
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) cur.v32[t][j >> 2][j & 3] = (live >> j & 1u) ? cur.v32[t][j >> 2][j & 3] : 0.f;
-        }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
+          floatx4_t x[2];
+          x[0] = *reinterpret_cast<const floatx4_t*>(v_lds + t * 16 * SG::kSegLds);
+          x[1] = *reinterpret_cast<const floatx4_t*>(v_lds + t * 16 * SG::kSegLds + 16);
+          if (!whole) {                                   // what lies behind the sequence's end may be anything
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j >> 2][j & 3] = (live >> j & 1u) ? x[j >> 2][j & 3] : 0.f;
+          }
           o[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int j = 0; j < 8; ++j) o[t] = mma_f32(cur.v32[t][j >> 2][j & 3], p[j], o[t]);
+          for (int j = 0; j < 8; ++j) o[t] = mma_f32(x[j >> 2][j & 3], p[j], o[t]);
         }
       } else if constexpr (CT == CT_BF16) {
+        uint4 mk = make_uint4(~0u, ~0u, ~0u, ~0u);
         if (!whole) {
-          uint32_t mk[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            mk[j] = ((live >> (2 * j) & 1u) ? 0xffffu : 0u) | ((live >> (2 * j + 1) & 1u) ? 0xffff0000u : 0u);
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-            cur.vf[t] = make_uint4(cur.vf[t].x & mk[0], cur.vf[t].y & mk[1], cur.vf[t].z & mk[2], cur.vf[t].w & mk[3]);
+          auto two = [&](int j) { return ((live >> j & 1u) ? 0xffffu : 0u) | ((live >> (j + 1) & 1u) ? 0xffff0000u : 0u); };
+          mk = make_uint4(two(0), two(2), two(4), two(6));
         }
         const uint4 hi = pack8(p);
         float r[8];
@@ -566,8 +625,10 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
         const uint4 lo = pack8(r);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          o[t] = mma_bf16(cur.vf[t], hi, floatx4_t{0.f, 0.f, 0.f, 0.f});
-          o[t] = mma_bf16(cur.vf[t], lo, o[t]);
+          uint4 x = *reinterpret_cast<const uint4*>(v_lds + t * 16 * SG::kSegLds);
+          if (!whole) x = make_uint4(x.x & mk.x, x.y & mk.y, x.z & mk.z, x.w & mk.w);
+          o[t] = mma_bf16(x, hi, floatx4_t{0.f, 0.f, 0.f, 0.f});
+          o[t] = mma_bf16(x, lo, o[t]);
         }
       } else {
         const uint4 off = make_uint4(kMinusMid2, kMinusMid2, kMinusMid2, kMinusMid2);
@@ -576,10 +637,10 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
         for (int w = 0; w < NW; ++w) {
           if (!whole) {                                   // what lies behind the sequence's end may be anything
             const int key = (16 * w + (NU >= 2 ? n : n & 7)) / NU;
-            cur.vp[w] = (live >> key & 1u) ? cur.vp[w] : 0u;
+            vp[w] = (live >> key & 1u) ? vp[w] : 0u;
           }
-          vstep[w] = __uint_as_float(cur.vp[w] << 16);
-          vmid[w] = fmaf(kCodeMid, vstep[w], __uint_as_float(cur.vp[w] & 0xffff0000u));
+          vstep[w] = __uint_as_float(vp[w] << 16);
+          vmid[w] = fmaf(kCodeMid, vstep[w], __uint_as_float(vp[w] & 0xffff0000u));
         }
         each<NU>([&](auto u_) {
           constexpr int u = decltype(u_)::value;
@@ -597,7 +658,7 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
           base = mma_bf16(off, lo, base);
 #pragma unroll
           for (int t = u * (NT / NU); t < (u + 1) * (NT / NU); ++t) {
-            const uint4 w = codes_bf16(cur.v4[t], cm, ce);
+            const uint4 w = codes_bf16(*reinterpret_cast<const uint32_t*>(v_lds + t * 16 * SG::kSegLds), cm, ce);
             o[t] = mma_bf16(w, hi, base);
             o[t] = mma_bf16(w, lo, o[t]);
           }
@@ -615,8 +676,6 @@ __global__ __launch_bounds__(kThreads) void k_attend(AttendArgs a, Plan pl) {
           for (int u = 0; u < NU; ++u) mid[u] = fmaf(mid[u], f, om[u]);
         }
       }
-      cur = next;
-      it = it_next;
     }
   }
 
