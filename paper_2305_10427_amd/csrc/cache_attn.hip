@@ -94,6 +94,7 @@ __device__ __forceinline__ uint32_t group_code(float x, float step, float least)
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kBlock = 32;                    // keys of an item
+constexpr int kUnit = 4;                      // blocks handed out together (128 keys: whole pages)
 constexpr int kListBlocks = 32;               // blocks whose items are listed at a time
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -157,13 +158,13 @@ constexpr float kCodeMid = 7.5f;
 constexpr uint32_t kMinusOff2 = 0xc180c180u;   // two bfloat16 of -16
 constexpr uint32_t kMinusMid2 = 0xc1bcc1bcu;   // two bfloat16 of -(16 + 7.5)
 
-// The tokens at position len - 1 of the tile's beams, where that lies in keys
-// [from, to): eight dimensions a lane.  In 4 bits a group's extremes come from
+// The tokens at position len - 1 of the tile's beams, where that lies in part
+// `split` of the keys: eight dimensions a lane.  In 4 bits a group's extremes come from
 // the four lanes that hold it.  The slots belong to one sequence each, so the
 // words that hold several tokens are read, changed and written by one lane.
 template <int CT, int DH>
-__device__ __forceinline__ void append_rows(const AttendArgs& a, int kv, int seq0, int beams, const int* s_len, int from,
-                                            int to) {
+__device__ __forceinline__ void append_rows(const AttendArgs& a, int kv, int seq0, int beams, const int* s_len, int split,
+                                            int splits) {
   const CacheView& c = a.c;
   constexpr int L8 = DH / 8;
   constexpr int G = DH >= 32 ? DH / 32 : 1;
@@ -171,7 +172,7 @@ __device__ __forceinline__ void append_rows(const AttendArgs& a, int kv, int seq
     const int i = i0 + threadIdx.x;
     const int r = i / (2 * L8), is_v = i / L8 & 1, d = 8 * (i & (L8 - 1));
     const int pos = r < beams ? s_len[r] - 1 : -1;
-    const int id = pos >= from && pos < to ? page_at(a.table, a.table_ld, seq0 + r, pos / c.ps, c.pages) : -1;
+    const int id = pos >= 0 && pos / (kUnit * kBlock) % splits == split ? page_at(a.table, a.table_ld, seq0 + r, pos / c.ps, c.pages) : -1;
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = 0.f;
@@ -356,14 +357,18 @@ template <int CT, int DH> struct Stage {
 
 template <int CT> constexpr int kSegLane = CT == CT_F32 ? 32 : CT == CT_BF16 ? 16 : 4;   // bytes of eight keys of a dimension
 
-// Split of the launch: beams per tile, tiles of a group, ranges of the keys.
+// Split of the launch: beams per tile, tiles of a group, parts of the keys.
+// Part z takes units z, z + splits, ...: behind the beams' common prefix a block
+// has an item for each of them, and every part gets its share of those.
 struct Plan {
-  int rows_per_tile, tiles, splits, blocks_per_split;
+  int rows_per_tile, tiles, splits;
 };
 
-// Waves a SIMD's registers are to hold.
+// Waves a SIMD is to hold (workgroups a CU), by registers and LDS.
 constexpr int waves_per_simd(int ct, int dh) {
-  return ct == CT_F32 ? (dh >= 128 ? 1 : dh == 64 ? 2 : 4) : dh >= 128 ? 2 : dh == 64 ? 3 : 4;
+  if (ct == CT_F32) return dh >= 128 ? 1 : dh == 64 ? 2 : dh == 32 ? 3 : 4;
+  if (ct == CT_BF16) return dh >= 128 ? 1 : dh == 64 ? 3 : 4;
+  return dh >= 128 ? 2 : dh == 64 ? 3 : 4;
 }
 
 template <int CT, int DH>
@@ -453,11 +458,12 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
 
   int longest = 0;
   for (int r = 0; r < beams; ++r) longest = max(longest, s_len[r]);
-  const int b_begin = split * pl.blocks_per_split;
-  const int b_end = min(b_begin + pl.blocks_per_split, (longest + kBlock - 1) / kBlock);
+  const int units = (longest + kUnit * kBlock - 1) / (kUnit * kBlock);
+  const int my_blocks = split < units ? (units - split + pl.splits - 1) / pl.splits * kUnit : 0;
+  auto block_of = [&](int i) { return ((i / kUnit) * pl.splits + split) * kUnit + i % kUnit; };   // my i-th
 
-  // the step's own token, by the workgroup whose range holds its position
-  if (a.new_k != nullptr) append_rows<CT, DH>(a, kv, seq0, beams, s_len, b_begin * kBlock, b_end * kBlock);
+  // the step's own token, by the workgroup whose part holds its position
+  if (a.new_k != nullptr) append_rows<CT, DH>(a, kv, seq0, beams, s_len, split, pl.splits);
 
   const uint32_t cm = CT == CT_INT4 ? in_vgpr(kCodeMask) : 0u, ce = CT == CT_INT4 ? in_vgpr(kCodeExp) : 0u;
   float m = -INFINITY, l = 0.f;
@@ -468,14 +474,14 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
 #pragma unroll
   for (int u = 0; u < NU; ++u) mid[u] = 0.f;
 
-  for (int b0 = b_begin; b0 < b_end; b0 += kListBlocks) {
+  for (int b0 = 0; b0 < my_blocks; b0 += kListBlocks) {
     // --- the items of up to kListBlocks blocks ---
-    const int nb = min(kListBlocks, b_end - b0);
+    const int nb = min(kListBlocks, my_blocks - b0);
     const int pairs = nb * beams;
     __syncthreads();
     for (int i = threadIdx.x; i < pairs; i += kThreads) {
       const int b = i / beams, r = i - b * beams;
-      const int j0 = (b0 + b) * kBlock;
+      const int j0 = block_of(b0 + b) * kBlock;
       const int nv = max(0, min(kBlock, s_len[r] - j0));
       const int s = seq0 + r;
       int id0 = -1, id1 = -1;
@@ -500,7 +506,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
           rows |= same ? 1u << o : 0u;
           if (same && o < r) lead = false;
         }
-        it = Item{t.x, t.y, b0 + b, rows << 16 | static_cast<uint32_t>(t.z)};
+        it = Item{t.x, t.y, block_of(b0 + b), rows << 16 | static_cast<uint32_t>(t.z)};
       }
       const uint64_t vote = __ballot(lead);
       if (lane == 0) s_cnt[wave] = __popcll(vote);
@@ -802,22 +808,23 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
 
 namespace {
 
-// Beams per tile: whole beams within 16 query rows.  Ranges of the keys: as many
-// as give the chip kWantWgs workgroups, while a range keeps two blocks for each
-// wave.
-constexpr int kWantWgs = 1024;
+// Beams per tile: whole beams within 16 query rows.  Parts of the keys: as many
+// as the chip holds workgroups at once, a second round of workgroups costing
+// more than it evens out (64 x 4 rows of 4,000 keys, 64 wide: bfloat16 73 us with
+// 768 workgroups, 103 with 1,024; 4 bits 55 and 71), while a part has at least
+// kMinUnits units.
+constexpr int kCus = 256;
+constexpr int kMinUnits = 1;
 Plan plan_attend(const CacheView& c, int n_seqs, int heads, int group, int max_len) {
   Plan p;
   const int G = heads / c.kv_heads;
   p.rows_per_tile = 16 / G < group ? 16 / G : group;
   p.tiles = (group + p.rows_per_tile - 1) / p.rows_per_tile;
-  const int blocks = (max_len + kBlock - 1) / kBlock;
+  const int units = (max_len + kUnit * kBlock - 1) / (kUnit * kBlock);
   const long long wgs = static_cast<long long>(n_seqs / group) * p.tiles * c.kv_heads;
-  long long want = (kWantWgs + wgs - 1) / wgs;
-  const long long most = (blocks + 2 * kWaves - 1) / (2 * kWaves);
-  if (want > most) want = most;
-  p.blocks_per_split = static_cast<int>((blocks + want - 1) / want);
-  p.splits = (blocks + p.blocks_per_split - 1) / p.blocks_per_split;
+  const long long want = kCus * waves_per_simd(c.type, c.dh) / wgs, most = units / kMinUnits;
+  p.splits = static_cast<int>(want < most ? want : most);
+  if (p.splits < 1) p.splits = 1;
   return p;
 }
 
