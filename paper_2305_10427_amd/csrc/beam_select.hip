@@ -284,15 +284,6 @@ __global__ __launch_bounds__(kRowWaves * kWave) void k_select_rows(SelectArgs a,
   if (unit < a.B * a.beam * parts) row_part<T>(a, w, parts, steps, unit, s_buf[wave], lane);
 }
 
-// Largest of the wave's values.
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-  v = max(v, dpp_u<kDppXor1>(v));
-  v = max(v, dpp_u<kDppXor2>(v));
-  v = max(v, dpp_u<kDppHalfMirror>(v));
-  v = max(v, dpp_u<kDppMirror>(v));
-  auto at = [&](int l) { return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), l)); };
-  return max(max(at(0), at(16)), max(at(32), at(48)));
-}
 // Order-preserving bits of a double (no NaN; -0 counts as 0).
 __device__ __forceinline__ u64 double_key(double d) {
   const u64 u = static_cast<u64>(__double_as_longlong(d + 0.0));

@@ -31,10 +31,6 @@ __device__ __forceinline__ int page_at(const int* table, int table_ld, int s, in
   return id >= 0 && id < pages ? id : -1;
 }
 
-__device__ __forceinline__ float load_any(const void* p, int bf16, size_t i) {
-  return bf16 ? Elt<bf16_t>::load(static_cast<const bf16_t*>(p), i) : Elt<float>::load(static_cast<const float*>(p), i);
-}
-
 // Index (in page-head blocks) of head h of page id of a layer.
 __device__ __forceinline__ size_t head_block(const CacheView& c, int layer, int id, int h) {
   return (static_cast<size_t>(layer) * c.pages + id) * c.kv_heads + h;
@@ -95,7 +91,6 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kBlock = 32;                    // keys of an item
 constexpr int kUnit = 4;                      // blocks handed out together (128 keys: whole pages)
-constexpr int kListBlocks = 32;               // blocks whose items are listed at a time
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Item {
@@ -104,6 +99,10 @@ struct Item {
   uint32_t rows_nv;                           // beams that own it (bits 16 ..), valid keys (low bits)
 };
 
+__device__ __forceinline__ void unpack_pair(uint32_t w, float& a, float& b) {
+  a = __uint_as_float(w << 16);
+  b = __uint_as_float(w & 0xffff0000u);
+}
 __device__ __forceinline__ float xor16_max(float v) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
@@ -141,9 +140,9 @@ __device__ __forceinline__ void take_off(float* v, uint4 p) {   // v -= p
 
 // The eight codes of a word as bfloat16 16 + code: a code fills the top of the
 // mantissa of 16 (exact), two of them in a shift and an AND-OR (whose masks are
-// kept in vector registers: the instruction takes no two constants).  The
-// offset is taken off inside the matrix product.  Scores take off 16; the
-// product with V takes off 16 + 7.5 and adds the middle of a group's range
+// kept in vector registers: the instruction takes no two constants).  Scores
+// take the offset off with the least value; the product with V takes off
+// 16 + 7.5 inside the matrix product and adds the middle of a group's range
 // apart, because its sum over many keys of differing sign would otherwise be a
 // small difference of large numbers.
 __device__ __forceinline__ uint4 codes_bf16(uint32_t w, uint32_t m, uint32_t e) {
@@ -155,86 +154,90 @@ __device__ __forceinline__ uint32_t in_vgpr(uint32_t x) {
 }
 constexpr uint32_t kCodeMask = 0x00780078u, kCodeExp = 0x41804180u;
 constexpr float kCodeMid = 7.5f;
-constexpr uint32_t kMinusOff2 = 0xc180c180u;   // two bfloat16 of -16
 constexpr uint32_t kMinusMid2 = 0xc1bcc1bcu;   // two bfloat16 of -(16 + 7.5)
 
-// The tokens at position len - 1 of the tile's beams, where that lies in part
-// `split` of the keys: eight dimensions a lane.  In 4 bits a group's extremes come from
-// the four lanes that hold it.  The slots belong to one sequence each, so the
-// words that hold several tokens are read, changed and written by one lane.
+// The append of a token, eight dimensions of its key or value a lane: entry i
+// of a tile is beam i / (2 DH / 8), the key or value, and the dimensions.
+template <int DH> struct AppendRow {
+  static constexpr int L8 = DH / 8;
+  int r, is_v, d, pos;
+  float x[8];
+  __device__ __forceinline__ void load(const AttendArgs& a, int kv, int seq0, int beams, int i) {
+    r = i / (2 * L8);
+    is_v = i / L8 & 1;
+    d = 8 * (i & (L8 - 1));
+    const bool in = r < beams;
+    r = in ? r : 0;
+    const void* src = is_v ? a.new_v : a.new_k;
+    const size_t x0 = static_cast<size_t>(seq0 + r) * a.new_ld + static_cast<size_t>(kv) * DH + d;
+    if (a.new_bf16) Vec16<bf16_t>::load(static_cast<const bf16_t*>(src), x0, x);
+    else load_n<float, 8>(static_cast<const float*>(src), x0, x);
+    pos = keys_of(a.lens, seq0 + r, a.max_len, a.table_ld, a.c.ps) - 1;
+    pos = in ? pos : -1;
+  }
+};
+
+// Writes it to page id (-1: not at all).  In 4 bits a group's extremes come from
+// the lanes that hold it.  The slots belong to one sequence each, so the words
+// that hold several tokens are read, changed and written by one lane.  All
+// lanes call this together.
 template <int CT, int DH>
-__device__ __forceinline__ void append_rows(const AttendArgs& a, int kv, int seq0, int beams, const int* s_len, int split,
-                                            int splits) {
+__device__ __forceinline__ void append_row(const AttendArgs& a, int kv, const AppendRow<DH>& row_, int id) {
   const CacheView& c = a.c;
-  constexpr int L8 = DH / 8;
   constexpr int G = DH >= 32 ? DH / 32 : 1;
-  for (int i0 = 0; i0 < beams * 2 * L8; i0 += kThreads) {
-    const int i = i0 + threadIdx.x;
-    const int r = i / (2 * L8), is_v = i / L8 & 1, d = 8 * (i & (L8 - 1));
-    const int pos = r < beams ? s_len[r] - 1 : -1;
-    const int id = pos >= 0 && pos / (kUnit * kBlock) % splits == split ? page_at(a.table, a.table_ld, seq0 + r, pos / c.ps, c.pages) : -1;
-    float x[8];
+  const float* x = row_.x;
+  const int is_v = row_.is_v, d = row_.d, pos = row_.pos;
+  float step = 0.f, least = 0.f;
+  if constexpr (CT == CT_INT4) {
+    float lo = x[0], hi = x[0], bad = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    if (id >= 0) {
-      const void* src = is_v ? a.new_v : a.new_k;
-      const size_t x0 = static_cast<size_t>(seq0 + r) * a.new_ld + static_cast<size_t>(kv) * DH + d;
-      if (a.new_bf16) Vec16<bf16_t>::load(static_cast<const bf16_t*>(src), x0, x);
-      else load_n<float, 8>(static_cast<const float*>(src), x0, x);
+    for (int e = 0; e < 8; ++e) {
+      lo = fminf(lo, x[e]);
+      hi = fmaxf(hi, x[e]);
+      bad = isfinite(x[e]) ? bad : 1.f;
     }
-    float step = 0.f, least = 0.f;
-    if constexpr (CT == CT_INT4) {
-      float lo = x[0], hi = x[0], bad = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        lo = fminf(lo, x[e]);
-        hi = fmaxf(hi, x[e]);
-        bad = isfinite(x[e]) ? bad : 1.f;
-      }
-      lo = fminf(lo, dpp_f<kDppXor1>(lo)); hi = fmaxf(hi, dpp_f<kDppXor1>(hi)); bad = fmaxf(bad, dpp_f<kDppXor1>(bad));
-      if constexpr (DH >= 32) {
-        lo = fminf(lo, dpp_f<kDppXor2>(lo)); hi = fmaxf(hi, dpp_f<kDppXor2>(hi)); bad = fmaxf(bad, dpp_f<kDppXor2>(bad));
-      }
-      group_params(lo, hi, bad == 0.f, step, least);
+    lo = fminf(lo, dpp_f<kDppXor1>(lo)); hi = fmaxf(hi, dpp_f<kDppXor1>(hi)); bad = fmaxf(bad, dpp_f<kDppXor1>(bad));
+    if constexpr (DH >= 32) {
+      lo = fminf(lo, dpp_f<kDppXor2>(lo)); hi = fmaxf(hi, dpp_f<kDppXor2>(hi)); bad = fmaxf(bad, dpp_f<kDppXor2>(bad));
     }
-    if (id < 0) continue;
-    const size_t hb = head_block(c, a.layer, id, kv);
-    const int t = pos & (c.ps - 1);
-    char* base = is_v ? c.v : c.k;
-    const size_t row = (hb * c.ps + t) * DH + d;            // K
-    if constexpr (CT == CT_INT4) {
-      uint32_t code[8];
+    group_params(lo, hi, bad == 0.f, step, least);
+  }
+  if (id < 0) return;
+  const size_t hb = head_block(c, a.layer, id, kv);
+  const int t = pos & (c.ps - 1);
+  char* base = is_v ? c.v : c.k;
+  const size_t row = (hb * c.ps + t) * DH + d;            // K
+  if constexpr (CT == CT_INT4) {
+    uint32_t code[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) code[e] = group_code(x[e], step, least);
-      if (d % 32 == 0)
-        reinterpret_cast<uint32_t*>(is_v ? c.vs : c.ks)[(hb * c.ps + t) * G + d / 32] =
-            (__float_as_uint(step) >> 16) | (__float_as_uint(least) & 0xffff0000u);
-      uint32_t* w = reinterpret_cast<uint32_t*>(base);
-      if (!is_v) {
-        uint32_t word = 0;
+    for (int e = 0; e < 8; ++e) code[e] = group_code(x[e], step, least);
+    if (d % 32 == 0)
+      reinterpret_cast<uint32_t*>(is_v ? c.vs : c.ks)[(hb * c.ps + t) * G + d / 32] =
+          (__float_as_uint(step) >> 16) | (__float_as_uint(least) & 0xffff0000u);
+    uint32_t* w = reinterpret_cast<uint32_t*>(base);
+    if (!is_v) {
+      uint32_t word = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) word |= code[e] << nibble_shift(e);
-        w[row >> 3] = word;
-      } else {
-        const int sh = nibble_shift(t & 7);
-        uint32_t old[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) old[e] = w[((hb * DH + d + e) * c.ps + t) >> 3];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[((hb * DH + d + e) * c.ps + t) >> 3] = (old[e] & ~(15u << sh)) | (code[e] << sh);
-      }
+      for (int e = 0; e < 8; ++e) word |= code[e] << nibble_shift(e);
+      w[row >> 3] = word;
     } else {
-      typedef typename std::conditional<CT == CT_F32, float, bf16_t>::type T;
-      T* w = reinterpret_cast<T*>(base);
-      if (!is_v) {
-        store8<T>(w, row, x);
-      } else {
+      const int sh = nibble_shift(t & 7);
+      uint32_t old[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) Elt<T>::store(w, (hb * DH + d + e) * c.ps + t, x[e]);
-      }
+      for (int e = 0; e < 8; ++e) old[e] = w[((hb * DH + d + e) * c.ps + t) >> 3];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[((hb * DH + d + e) * c.ps + t) >> 3] = (old[e] & ~(15u << sh)) | (code[e] << sh);
+    }
+  } else {
+    typedef typename std::conditional<CT == CT_F32, float, bf16_t>::type T;
+    T* w = reinterpret_cast<T*>(base);
+    if (!is_v) {
+      store8<T>(w, row, x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) Elt<T>::store(w, (hb * DH + d + e) * c.ps + t, x[e]);
     }
   }
-  __threadfence_block();
 }
 
 // out = o / l for four dimensions of a row; a row without keys is zero.
@@ -283,7 +286,8 @@ template <int CT, int DH> struct Stage {
   static constexpr int kPiece = CT == CT_INT4 ? 8 : 16;
   static constexpr int kRowLds = kRow >= 32 ? kRow + 16 : kRow;
   static constexpr int kSegLds = kSeg > 16 ? kSeg + 16 : kSeg;
-  static constexpr int kBytes = kBlock * kRowLds + DH * kSegLds;                            // of a wave
+  static constexpr int kOut = 16 * (DH + 4) * 4;                                            // of a wave's output
+  static constexpr int kBytes = kBlock * kRowLds + DH * kSegLds > kOut ? kBlock * kRowLds + DH * kSegLds : kOut;
   static constexpr int NK = (kBlock * kRow / kPiece + kWave - 1) / kWave;                   // pieces a lane
   static constexpr int NV = (DH * kSeg / kPiece + kWave - 1) / kWave;
   static constexpr int PK = kRow / kPiece, PH = kSeg / 2 / kPiece;                          // pieces of a key, of half a segment
@@ -390,80 +394,150 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
   const int seq0 = grp * a.group + beam0;
   const int ps = c.ps;
 
-  // the lists, the items' data and at the end the waves' outputs share their LDS
+  // each wave's own: its list of items, the data of one, and at the end its output
   typedef Stage<CT, DH> SG;
-  struct Lists {
-    Item item[kListBlocks * 16];
+  struct WaveLds {
+    Item item[kWave];
+    int4 tup[kWave];
     union {
-      int4 tup[kListBlocks * 16];
-      char stage[kWaves][SG::kBytes];
+      char stage[SG::kBytes];
+      float out[16][DH + 4];
     };
   };
-  typedef float Outs[kWaves][16][DH + 4];
-  __shared__ __align__(16) char s_mem[sizeof(Lists) > sizeof(Outs) ? sizeof(Lists) : sizeof(Outs)];
-  Item* s_item = reinterpret_cast<Lists*>(s_mem)->item;
-  int4* s_tup = reinterpret_cast<Lists*>(s_mem)->tup;
-  Outs& s_o = *reinterpret_cast<Outs*>(s_mem);
-  char* lds = reinterpret_cast<Lists*>(s_mem)->stage[wave];
+  __shared__ __align__(16) char s_mem[kWaves * sizeof(WaveLds)];
+  WaveLds* s_wave = reinterpret_cast<WaveLds*>(s_mem);
+  WaveLds& my = s_wave[wave];
+  char* lds = my.stage;
   const char* k_lds = lds + n * SG::kRowLds + (CT == CT_INT4 ? (DH >= 32 ? 4 * g : 4 * (g & 1)) : CT == CT_BF16 && DH < 32 ? 16 * (g & 1) : 16 * g);
   const char* v_lds = lds + kBlock * SG::kRowLds + n * SG::kSegLds + kSegLane<CT> * g;
-  __shared__ int s_len[16];
-  __shared__ int s_cnt[kWaves];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
 
-  if (threadIdx.x < 16)
-    s_len[threadIdx.x] = static_cast<int>(threadIdx.x) < beams ? keys_of(a.lens, seq0 + threadIdx.x, a.max_len, a.table_ld, ps) : 0;
+  // --- what depends on nothing else is requested first ---
+  AppendRow<DH> ap;
+  if (a.new_k != nullptr) ap.load(a, kv, seq0, beams, threadIdx.x);
+  // a list: the lane's (block, beam) of kWave / beams blocks, their pages
+  const int list_blocks = kWave / beams;
+  const int b_l = lane / beams, r_l = lane - b_l * beams;
+  const bool pair = b_l < list_blocks;
+  auto block_of = [&](int i) { return ((i / kUnit) * pl.splits + split) * kUnit + i % kUnit; };   // my i-th block
+  int id0 = -1, id1 = -1;
+  auto fetch = [&](int list) {
+    const int j = block_of(list * list_blocks + b_l) * kBlock / ps;
+    id0 = pair && j < a.table_ld ? page_at(a.table, a.table_ld, seq0 + r_l, j, c.pages) : -1;
+    id1 = ps > 16 ? id0 : pair && j + 1 < a.table_ld ? page_at(a.table, a.table_ld, seq0 + r_l, j + 1, c.pages) : -1;
+  };
+  fetch(0);
+  const int len = pair ? keys_of(a.lens, seq0 + r_l, a.max_len, a.table_ld, ps) : 0;
   // queries: lane (n, g) holds dimensions 32 u + 8 g .. + 7 (float: 16 u + 4 g .. + 3) of row n
   const int beam_n = n / G;
   const bool row_ok = beam_n < beams;
   const size_t q0 = static_cast<size_t>(seq0 + (row_ok ? beam_n : 0)) * a.q_ld +
                     (static_cast<size_t>(kv) * G + (row_ok ? n % G : 0)) * DH;
+  constexpr int QE = CT == CT_F32 ? 4 : 8, QU = CT == CT_F32 ? DH / 16 : NU;
+  const int q_at = CT == CT_F32 ? 4 * g : DH >= 32 ? 8 * g : 8 * (g & 1);
+  float qv[QU][QE];
+  if (a.q_bf16) {
+#pragma unroll
+    for (int u = 0; u < QU; ++u) {
+      const bf16_t* p = static_cast<const bf16_t*>(a.q) + q0 + 4 * QE * u + q_at;
+      if constexpr (QE == 8) {
+        Vec16<bf16_t>::load(p, 0, qv[u]);
+      } else {
+        const uint2 w = *reinterpret_cast<const uint2*>(p);
+        unpack_pair(w.x, qv[u][0], qv[u][1]);
+        unpack_pair(w.y, qv[u][2], qv[u][3]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < QU; ++u) load_n<float, QE>(static_cast<const float*>(a.q), q0 + 4 * QE * u + q_at, qv[u]);
+  }
+  int ap_id = -1;
+  auto my_slot = [&](int pos) { return pos >= 0 && pos / (kUnit * kBlock) % pl.splits == split; };
+  if (a.new_k != nullptr && my_slot(ap.pos)) ap_id = page_at(a.table, a.table_ld, seq0 + ap.r, ap.pos / ps, c.pages);
+
   const float s2 = a.scale * kLog2e;                  // scores come out in units of log 2
   uint4 qf[CT == CT_F32 ? 1 : NU][3];
   floatx4_t q32[NF];
   float qsum[NU];                                     // 4 bits: sum of the row's queries over a group
-  floatx4_t qoff[NU];                                 // and -16 times it
   if constexpr (CT == CT_F32) {
 #pragma unroll
     for (int u = 0; u < NF; ++u)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) q32[u][e] = row_ok ? s2 * load_any(a.q, a.q_bf16, q0 + 16 * u + 4 * g + e) : 0.f;
+      for (int e = 0; e < 4; ++e) q32[u][e] = row_ok ? s2 * qv[u][e] : 0.f;
   } else {
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool in = row_ok && (DH >= 32 || g < 2);
-        v[e] = in ? s2 * load_any(a.q, a.q_bf16, q0 + 32 * u + 8 * g + e) : 0.f;
-      }
+      float* v = qv[u];
       float sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += v[e];
+      for (int e = 0; e < 8; ++e) {
+        v[e] = row_ok && (DH >= 32 || g < 2) ? s2 * v[e] : 0.f;
+        sum += v[e];
+      }
       qsum[u] = xor32_sum(xor16_sum(sum));
 #pragma unroll
       for (int part = 0; part < 3; ++part) {
         qf[u][part] = pack8(v);
         take_off(v, qf[u][part]);
       }
-      if constexpr (CT == CT_INT4) {
-        const uint4 off = make_uint4(kMinusOff2, kMinusOff2, kMinusOff2, kMinusOff2);
-        qoff[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int part = 0; part < 3; ++part) qoff[u] = mma_bf16(off, qf[u][part], qoff[u]);
-      }
     }
   }
-  __syncthreads();
-
-  int longest = 0;
-  for (int r = 0; r < beams; ++r) longest = max(longest, s_len[r]);
+  const int longest = static_cast<int>(wave_max_u32(static_cast<uint32_t>(len)));
   const int units = (longest + kUnit * kBlock - 1) / (kUnit * kBlock);
   const int my_blocks = split < units ? (units - split + pl.splits - 1) / pl.splits * kUnit : 0;
-  auto block_of = [&](int i) { return ((i / kUnit) * pl.splits + split) * kUnit + i % kUnit; };   // my i-th
+  const int lists = (my_blocks + list_blocks - 1) / list_blocks;
+
+  // The items of list `list` (every wave makes the same one, without a word to
+  // the others) from the pages that have been fetched; then the next ones are.
+  auto make_list = [&](int list) -> int {
+    const int block = block_of(list * list_blocks + b_l);
+    const int nv = max(0, min(kBlock, len - block * kBlock));
+    const int4 t = make_int4(nv > 0 ? id0 : -1, nv > 16 ? id1 : -1, nv, 0);
+    wave_lds_sync();
+    my.tup[lane] = t;
+    wave_lds_sync();
+    bool lead = t.x >= 0 || t.y >= 0;
+    uint32_t rows = 0;
+    for (int o = 0; o < beams; ++o) {
+      const int4 x = my.tup[min(b_l * beams + o, kWave - 1)];
+      const bool same = x.x == t.x && x.y == t.y && x.z == t.z;
+      rows |= same ? 1u << o : 0u;
+      if (same && o < r_l) lead = false;
+    }
+    const uint64_t vote = __ballot(lead);
+    if (lead) my.item[__popcll(vote & ((1ull << lane) - 1))] = Item{t.x, t.y, block, rows << 16 | static_cast<uint32_t>(nv)};
+    wave_lds_sync();
+    if (list + 1 < lists) fetch(list + 1);
+    return __popcll(vote);
+  };
+  int list = 0, n_items = lists > 0 ? make_list(0) : 0, at_item = wave;
+  // The wave's next item: every kWaves-th of all lists'.
+  auto seek = [&](Item& it) -> bool {
+    while (at_item >= n_items) {
+      at_item -= n_items;
+      if (++list >= lists) return false;
+      n_items = make_list(list);
+    }
+    const Item x = my.item[at_item];
+    at_item += kWaves;
+    it.id0 = __builtin_amdgcn_readfirstlane(x.id0);
+    it.id1 = __builtin_amdgcn_readfirstlane(x.id1);
+    it.block = __builtin_amdgcn_readfirstlane(x.block);
+    it.rows_nv = __builtin_amdgcn_readfirstlane(x.rows_nv);
+    return true;
+  };
 
   // the step's own token, by the workgroup whose part holds its position
-  if (a.new_k != nullptr) append_rows<CT, DH>(a, kv, seq0, beams, s_len, split, pl.splits);
+  if (a.new_k != nullptr) {
+    append_row<CT, DH>(a, kv, ap, ap_id);
+    for (int i = kThreads; i < beams * 2 * AppendRow<DH>::L8; i += kThreads) {
+      ap.load(a, kv, seq0, beams, i + threadIdx.x);
+      append_row<CT, DH>(a, kv, ap, my_slot(ap.pos) ? page_at(a.table, a.table_ld, seq0 + ap.r, ap.pos / ps, c.pages) : -1);
+    }
+    __threadfence_block();
+    __syncthreads();
+  }
 
   const uint32_t cm = CT == CT_INT4 ? in_vgpr(kCodeMask) : 0u, ce = CT == CT_INT4 ? in_vgpr(kCodeExp) : 0u;
   float m = -INFINITY, l = 0.f;
@@ -474,59 +548,15 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
 #pragma unroll
   for (int u = 0; u < NU; ++u) mid[u] = 0.f;
 
-  for (int b0 = 0; b0 < my_blocks; b0 += kListBlocks) {
-    // --- the items of up to kListBlocks blocks ---
-    const int nb = min(kListBlocks, my_blocks - b0);
-    const int pairs = nb * beams;
-    __syncthreads();
-    for (int i = threadIdx.x; i < pairs; i += kThreads) {
-      const int b = i / beams, r = i - b * beams;
-      const int j0 = block_of(b0 + b) * kBlock;
-      const int nv = max(0, min(kBlock, s_len[r] - j0));
-      const int s = seq0 + r;
-      int id0 = -1, id1 = -1;
-      if (nv > 0) id0 = page_at(a.table, a.table_ld, s, j0 / ps, c.pages);
-      if (nv > 16) id1 = ps > 16 ? id0 : page_at(a.table, a.table_ld, s, j0 / ps + 1, c.pages);
-      s_tup[i] = make_int4(id0, id1, nv, 0);
-    }
-    __syncthreads();
-    int n_items = 0;
-    for (int i0 = 0; i0 < pairs; i0 += kThreads) {
-      const int i = i0 + threadIdx.x;
-      bool lead = false;
-      Item it;
-      if (i < pairs) {
-        const int b = i / beams, r = i - b * beams;
-        const int4 t = s_tup[i];
-        lead = t.z > 0 && (t.x >= 0 || t.y >= 0);
-        uint32_t rows = 0;
-        for (int o = 0; o < beams; ++o) {
-          const int4 x = s_tup[b * beams + o];
-          const bool same = x.x == t.x && x.y == t.y && x.z == t.z;
-          rows |= same ? 1u << o : 0u;
-          if (same && o < r) lead = false;
-        }
-        it = Item{t.x, t.y, block_of(b0 + b), rows << 16 | static_cast<uint32_t>(t.z)};
-      }
-      const uint64_t vote = __ballot(lead);
-      if (lane == 0) s_cnt[wave] = __popcll(vote);
-      __syncthreads();
-      int at = n_items;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        at += w < wave ? s_cnt[w] : 0;
-        n_items += s_cnt[w];
-      }
-      if (lead) s_item[at + __popcll(vote & ((1ull << lane) - 1))] = it;
-      __syncthreads();
-    }
-
-    // a wave's items: one in LDS, the next one on its way in registers
+  // a wave's items: one in LDS, the next one on its way in registers
+  {
     Stage<CT, DH> st;
     uint32_t kp[SG::NW], vp[SG::NW];
-    if (wave < n_items) st.load(c, a.layer, kv, s_item[wave], lane);
-    for (int i = wave; i < n_items; i += kWaves) {
-      const Item it = s_item[i];
+    Item next;
+    bool more = seek(next);
+    if (more) st.load(c, a.layer, kv, next, lane);
+    while (more) {
+      const Item it = next;
       wave_lds_sync();                                   // the wave is done with the item before
       st.store(lds, lane, ps);
 #pragma unroll
@@ -534,7 +564,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
         if constexpr (CT == CT_INT4) kp[w] = st.kp[w], vp[w] = st.vp[w];
       }
       wave_lds_sync();
-      if (i + kWaves < n_items) st.load(c, a.layer, kv, s_item[i + kWaves], lane);
+      more = seek(next);
+      if (more) st.load(c, a.layer, kv, next, lane);
       const int nv = it.rows_nv & 0xffff;
       const bool own = row_ok && ((it.rows_nv >> 16) >> beam_n & 1u);
       const bool whole = nv == kBlock && it.id0 >= 0 && it.id1 >= 0;
@@ -545,7 +576,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
           kstep[w] = __uint_as_float(kp[w] << 16);
-          kleast[w] = __uint_as_float(kp[w] & 0xffff0000u);
+          kleast[w] = fmaf(-16.f, kstep[w], __uint_as_float(kp[w] & 0xffff0000u));   // less the codes' offset
         }
       }
       each<2>([&](auto t_) {
@@ -568,7 +599,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
         } else {
           each<NU>([&](auto u_) {
             constexpr int u = decltype(u_)::value;
-            floatx4_t x = qoff[u];
+            floatx4_t x = {0.f, 0.f, 0.f, 0.f};
             const uint4 w = codes_bf16(*reinterpret_cast<const uint32_t*>(k_lds + t * 16 * SG::kRowLds + 16 * u), cm, ce);
 #pragma unroll
             for (int part = 0; part < 3; ++part) x = mma_bf16(w, qf[u][part], x);
@@ -697,13 +728,13 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
         for (int e = 0; e < 4; ++e) acc[t][e] += x;
     }
   }
-  __syncthreads();                                    // every wave is done with the lists
+  wave_lds_sync();                                    // the wave is done with its last item
   if (g == 0) {
     s_m[wave][n] = m;
     s_l[wave][n] = l;
   }
 #pragma unroll
-  for (int t = 0; t < NT; ++t) *reinterpret_cast<floatx4_t*>(&s_o[wave][n][16 * t + 4 * g]) = acc[t];
+  for (int t = 0; t < NT; ++t) *reinterpret_cast<floatx4_t*>(&my.out[n][16 * t + 4 * g]) = acc[t];
   __syncthreads();
   const int rows = beams * G;
   const int parts = a.n_seqs * a.heads;
@@ -718,7 +749,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
     for (int w = 0; w < kWaves; ++w) {
       const float f = s_m[w][r] == -INFINITY && !(s_l[w][r] != 0.f) ? 0.f : __builtin_amdgcn_exp2f(s_m[w][r] - mt);
       lt = fmaf(s_l[w][r], f, lt);
-      const floatx4_t x = *reinterpret_cast<const floatx4_t*>(&s_o[w][r][d]);
+      const floatx4_t x = *reinterpret_cast<const floatx4_t*>(&s_wave[w].out[r][d]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = fmaf(x[e], f, o[e]);
     }
