@@ -6,7 +6,6 @@ library is missing or fails, calls raise.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import NamedTuple, Optional, Sequence
@@ -404,22 +403,19 @@ class PageMoves(NamedTuple):
     status: object
 
 
-def _scope(dev, stream):
-    """Makes `stream` (default: the current stream of `dev`) current, so that outputs and scratch belong to it."""
+def _on(dev, stream, launch):
+    """launch(stream handle) with `stream` (default: the current stream of `dev`) made current, so that outputs and
+    scratch belong to it."""
     import torch
     if stream is not None:
         if stream.device != dev:
             raise PdError(1, f"the stream is on {stream.device}, the tensors are on {dev}")
-        return torch.cuda.stream(stream)
-    if dev.type == "cuda" and dev.index != torch.cuda.current_device():
-        return torch.cuda.device(dev)
-    return contextlib.nullcontext()
-
-
-def _raw_stream(dev) -> int:
-    """Handle of the current stream of dev (torch.cuda.current_stream(dev).cuda_stream without making a Stream)."""
-    import torch
-    return torch._C._cuda_getCurrentRawStream(dev.index)
+        with torch.cuda.stream(stream):
+            return launch(stream.cuda_stream)
+    if dev.index != torch._C._cuda_getDevice():
+        with torch.cuda.device(dev):
+            return launch(torch._C._cuda_getCurrentRawStream(dev.index))
+    return launch(torch._C._cuda_getCurrentRawStream(dev.index))
 
 
 def _tensor(name, t, dtypes, shape, dev, contiguous=True):
@@ -443,6 +439,8 @@ def _tensor(name, t, dtypes, shape, dev, contiguous=True):
 
 def _rows(name, t):
     """Elements from one row of a 3-D tensor to the next: the last two dimensions packed, rows of any distance."""
+    if t.is_contiguous():
+        return t.shape[1] * t.shape[2]
     n = t.shape[2]
     if (t.shape[2] > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != n):
         raise PdError(1, f"the rows of {name} must be contiguous")
@@ -470,17 +468,20 @@ def beam_select(logits, scores, lens, done, *, eos_id: int = C.EOS_ID, pad_id: i
     dt = 1 if logits.dtype == torch.bfloat16 else 0
     n = ctypes.c_size_t()
     _check(L.pd_beam_select_bytes(dt, B, K, V, ctypes.byref(n)))
-    with _scope(dev, stream):
+
+    def launch(handle):
         out = torch.empty_like(scores)
         ints = torch.empty((5, B, K), dtype=torch.int32, device=dev)
         flags = torch.empty((B,), dtype=torch.int32, device=dev)
         ws = torch.empty((n.value,), dtype=torch.uint8, device=dev)
         at, step = ints.data_ptr(), 4 * B * K
         _check(L.pd_beam_select(logits.data_ptr(), dt, ld, B, K, V, scores.data_ptr(), lens.data_ptr(),
-                                done.data_ptr(), max_len.data_ptr() if max_len is not None else None, eos_id, pad_id,
+                                done.data_ptr(), None if max_len is None else max_len.data_ptr(), eos_id, pad_id,
                                 alpha, out.data_ptr(), at, at + step, at + 2 * step, at + 3 * step, at + 4 * step,
-                                flags.data_ptr(), ws.data_ptr(), n.value, _raw_stream(dev)))
-    return BeamStep(out, *ints.unbind(0), flags)
+                                flags.data_ptr(), ws.data_ptr(), n.value, handle))
+        return BeamStep(out, *ints.unbind(0), flags)
+
+    return _on(dev, stream, launch)
 
 
 class PagedCache:
@@ -523,9 +524,13 @@ class PagedCache:
 
     def _table(self, table, lens):
         import torch
-        _tensor("table", table, (torch.int32,), (None, None), self.device)
-        _tensor("lens", lens, (torch.int32,), (table.shape[0],), self.device)
-        return table.shape
+        i32 = (torch.int32,)
+        shape = table.shape
+        if len(shape) != 2:
+            _tensor("table", table, i32, (None, None), self.device)
+        _tensor("table", table, i32, shape, self.device)
+        _tensor("lens", lens, i32, shape[:1], self.device)
+        return shape
 
     def _bytes(self, fn, *sizes):
         key = (fn,) + sizes
@@ -543,9 +548,10 @@ class PagedCache:
         import torch
         L = load_library()
         S, ld = self._table(table, lens)
+        dev, dh = self.device, self.head_dim
         types = (torch.float32, torch.bfloat16)
-        _tensor("q", q, types, (S, None, self.head_dim), self.device, contiguous=False)
-        H = q.shape[1]
+        H = q.shape[1] if len(q.shape) == 3 else None
+        _tensor("q", q, types, (S, H, dh), dev, contiguous=False)
         odt = q.dtype if out_dtype is None else out_dtype
         if odt not in types:
             raise PdError(1, "out_dtype must be torch.float32 or torch.bfloat16")
@@ -554,67 +560,81 @@ class PagedCache:
         kp = vp = None
         ndt = nld = 0
         if new_k is not None:
-            for name, x in (("new_k", new_k), ("new_v", new_v)):
-                _tensor(name, x, types, (S, self.kv_heads, self.head_dim), self.device, contiguous=False)
+            shape = (S, self.kv_heads, dh)
+            _tensor("new_k", new_k, types, shape, dev, contiguous=False)
+            _tensor("new_v", new_v, types, shape, dev, contiguous=False)
             nld = _rows("new_k", new_k)
             if new_v.dtype != new_k.dtype or _rows("new_v", new_v) != nld:
                 raise PdError(1, "new_k and new_v must have the same type and row distance")
             kp, vp, ndt = new_k.data_ptr(), new_v.data_ptr(), int(new_k.dtype == torch.bfloat16)
         top = ld * self.page_size if max_len is None else max_len
         n = self._bytes("pd_cache_attend_bytes", H, S, group, top)
-        with _scope(self.device, stream):
-            out = torch.empty((S, H, self.head_dim), dtype=odt, device=self.device)
-            ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+
+        def launch(handle):
+            out = torch.empty((S, H, dh), dtype=odt, device=dev)
+            ws = torch.empty((n,), dtype=torch.uint8, device=dev).data_ptr() if n else None
             _check(L.pd_cache_attend(self._p, layer, q.data_ptr(), int(q.dtype == torch.bfloat16), _rows("q", q), H, kp,
                                      vp, ndt, nld, table.data_ptr(), ld, lens.data_ptr(), S, group, top,
-                                     self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
-                                     int(odt == torch.bfloat16), H * self.head_dim, ws.data_ptr() if n else None, n,
-                                     _raw_stream(self.device)))
-        return out
+                                     dh ** -0.5 if scale is None else scale, out.data_ptr(),
+                                     int(odt == torch.bfloat16), H * dh, ws, n, handle))
+            return out
+
+        return _on(dev, stream, launch)
 
     def read(self, table, lens, first, *, layer: int = 0, count: int = 1, stream=None):
         """Values held at positions first .. first + count - 1 of each sequence, float32
         ([S, count, kv_heads, head_dim] of keys, of values); zero outside the sequence."""
         import torch
         S, ld = self._table(table, lens)
-        _tensor("first", first, (torch.int32,), (S,), self.device)
-        with _scope(self.device, stream):
-            k, v = (torch.empty((S, max(count, 1), self.kv_heads, self.head_dim), dtype=torch.float32, device=self.device)
-                    for _ in range(2))
+        dev = self.device
+        _tensor("first", first, (torch.int32,), (S,), dev)
+
+        def launch(handle):
+            shape = (S, max(count, 1), self.kv_heads, self.head_dim)
+            k = torch.empty(shape, dtype=torch.float32, device=dev)
+            v = torch.empty(shape, dtype=torch.float32, device=dev)
             _check(load_library().pd_cache_read(self._p, layer, table.data_ptr(), ld, lens.data_ptr(), S,
-                                                first.data_ptr(), count, k.data_ptr(), v.data_ptr(),
-                                                _raw_stream(self.device)))
-        return k, v
+                                                first.data_ptr(), count, k.data_ptr(), v.data_ptr(), handle))
+            return k, v
+
+        return _on(dev, stream, launch)
 
     def fork(self, table, lens, parents, *, grow: bool = True, stream=None) -> PageFork:
         """The table of the sequences whose parents are given (-1: empty), with a slot for the next token if grow
         (pd_pages_fork)."""
         import torch
         S, ld = self._table(table, lens)
-        _tensor("parents", parents, (torch.int32,), (None,), self.device)
+        dev = self.device
+        _tensor("parents", parents, (torch.int32,), parents.shape if len(parents.shape) == 1 else (None,), dev)
         n_out = parents.shape[0]
         n = self._bytes("pd_pages_bytes", n_out)
-        with _scope(self.device, stream):
-            new = torch.empty((n_out, ld), dtype=torch.int32, device=self.device)
-            rest = torch.empty(n_out + self.pages + 2, dtype=torch.int32, device=self.device)
-            out_lens, refs, status = rest.split((n_out, self.pages, 2))
-            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+
+        def launch(handle):
+            new = torch.empty((n_out, ld), dtype=torch.int32, device=dev)
+            rest = torch.empty((n_out + self.pages + 2,), dtype=torch.int32, device=dev)
+            ws = torch.empty((n,), dtype=torch.uint8, device=dev)
+            at = rest.data_ptr()
             _check(load_library().pd_pages_fork(self._p, table.data_ptr(), ld, lens.data_ptr(), S, parents.data_ptr(),
-                                                n_out, int(grow), new.data_ptr(), out_lens.data_ptr(), refs.data_ptr(),
-                                                status.data_ptr(), ws.data_ptr(), n, _raw_stream(self.device)))
-        return PageFork(new, out_lens, refs, status)
+                                                n_out, int(grow), new.data_ptr(), at, at + 4 * n_out,
+                                                at + 4 * (n_out + self.pages), ws.data_ptr(), n, handle))
+            return PageFork(new, *rest.split_with_sizes((n_out, self.pages, 2)))
+
+        return _on(dev, stream, launch)
 
     def compact(self, table, lens, *, stream=None) -> PageMoves:
         """Moves the pages in use to the front of the pool (pd_pages_compact)."""
         import torch
         S, ld = self._table(table, lens)
+        dev = self.device
         n = self._bytes("pd_pages_bytes", S)
-        with _scope(self.device, stream):
-            new = torch.empty((S, ld), dtype=torch.int32, device=self.device)
-            rest = torch.empty(self.pages + 2, dtype=torch.int32, device=self.device)
-            remap, status = rest.split((self.pages, 2))
-            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-            _check(load_library().pd_pages_compact(self._p, table.data_ptr(), ld, lens.data_ptr(), S, new.data_ptr(),
-                                                   remap.data_ptr(), status.data_ptr(), ws.data_ptr(), n,
-                                                   _raw_stream(self.device)))
-        return PageMoves(new, remap, status)
+
+        def launch(handle):
+            new = torch.empty((S, ld), dtype=torch.int32, device=dev)
+            rest = torch.empty((self.pages + 2,), dtype=torch.int32, device=dev)
+            ws = torch.empty((n,), dtype=torch.uint8, device=dev)
+            at = rest.data_ptr()
+            _check(load_library().pd_pages_compact(self._p, table.data_ptr(), ld, lens.data_ptr(), S, new.data_ptr(), at,
+                                                   at + 4 * self.pages, ws.data_ptr(), n, handle))
+            return PageMoves(new, *rest.split_with_sizes((self.pages, 2)))
+
+        return _on(dev, stream, launch)
