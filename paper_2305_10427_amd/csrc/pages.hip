@@ -77,56 +77,101 @@ __device__ __forceinline__ int parent_of(const PagesArgs& a, int s, int& len) {
   return p;
 }
 
+// A plan is one workgroup's work: a page gets its number by a prefix sum over the
+// pool.  What bounds it is latency, so pools and tables that fit (most do: 8192
+// pages, 2048 sequences) are counted in LDS, with the loads of kBatch entries
+// under way at a time; larger ones in global memory.
+constexpr int kLdsPages = 8192, kLdsSeqs = 2048;
+constexpr int kBatch = 4;
+
+template <bool LDS> __device__ __forceinline__ int counted(const int* p) {   // a value that atomics have made
+  return LDS ? *p : __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <bool LDS>
 __global__ __launch_bounds__(kPlanThreads) void k_fork_plan(PagesArgs a, PagesWs w) {
   const int t = threadIdx.x, P = a.c.pages, ps = a.c.ps, ld = a.table_ld;
   __shared__ int s_scan[kPlanWaves];
   __shared__ int s_full;
-  // no references yet
+  __shared__ int s_refs[LDS ? kLdsPages : 1], s_writers[LDS ? kLdsPages : 1], s_first[LDS ? kLdsPages : 1];
+  __shared__ int2 s_seq[LDS ? kLdsSeqs : 1], s_need[LDS ? kLdsSeqs : 1];
+  int* refs = LDS ? s_refs : a.refs;
+  int* writers = LDS ? s_writers : w.writers;
+  int* first = LDS ? s_first : w.first;
+  int2* need_list = LDS ? s_need : w.copies;          // (page to copy or -1, sequence)
+  auto sync = [&]() {
+    if constexpr (!LDS) __threadfence();
+    __syncthreads();
+  };
+  // no references yet; each sequence's parent (-1: none) and its length
+  if constexpr (LDS) {
+    for (int s = t; s < a.n_out; s += kPlanThreads) {
+      int len;
+      const int p = parent_of(a, s, len);
+      s_seq[s] = make_int2(p, len);
+    }
+  }
   for (int p = t; p < P; p += kPlanThreads) {
-    a.refs[p] = 0;
-    w.writers[p] = 0;
-    w.first[p] = 0x7fffffff;
+    refs[p] = 0;
+    writers[p] = 0;
+    first[p] = 0x7fffffff;
   }
   if (t == 0) s_full = 0;
-  __threadfence();
-  __syncthreads();
-  // the parents' pages, counted
-  for (long long i = t; i < static_cast<long long>(a.n_out) * ld; i += kPlanThreads) {
-    const int s = static_cast<int>(i / ld), j = static_cast<int>(i - static_cast<long long>(s) * ld);
-    int len;
-    const int p = parent_of(a, s, len);
-    int id = -1;
-    if (p >= 0 && j < pages_of(len, ps)) id = a.table[static_cast<size_t>(p) * ld + j];
-    if (id < 0 || id >= P) id = -1;
-    if (id >= 0) atomicAdd(&a.refs[id], 1);
-    a.out_table[i] = id;
-    if (j == 0) a.out_lens[s] = len + (p >= 0 && a.grow ? 1 : 0);
-    if (id >= 0 && a.grow && len % ps != 0 && j == len / ps) {
-      atomicAdd(&w.writers[id], 1);
-      atomicMin(&w.first[id], s);
+  sync();
+  auto seq = [&](int s, int& len) -> int {
+    if constexpr (LDS) {
+      len = s_seq[s].y;
+      return s_seq[s].x;
     }
-    if (j == 0 && p >= 0 && a.grow && len == ld * ps) atomicAdd(&s_full, 1);   // the table row has no place for a page
+    return parent_of(a, s, len);
+  };
+  // the parents' pages, counted
+  const long long entries = static_cast<long long>(a.n_out) * ld;
+  for (long long i0 = t; i0 < entries; i0 += kBatch * kPlanThreads) {
+    int id[kBatch], s[kBatch], j[kBatch], len[kBatch], p[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const long long i = i0 + k * kPlanThreads;
+      const bool in = i < entries;
+      if constexpr (LDS) s[k] = in ? static_cast<int>(i) / ld : 0;
+      else s[k] = in ? static_cast<int>(i / ld) : 0;
+      j[k] = static_cast<int>(i - static_cast<long long>(s[k]) * ld);
+      p[k] = seq(s[k], len[k]);
+      const bool there = in && p[k] >= 0 && j[k] < pages_of(len[k], ps);
+      id[k] = there ? a.table[static_cast<size_t>(p[k]) * ld + j[k]] : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const long long i = i0 + k * kPlanThreads;
+      if (i >= entries) continue;
+      if (id[k] < 0 || id[k] >= P) id[k] = -1;
+      a.out_table[i] = id[k];
+      if (id[k] >= 0) atomicAdd(&refs[id[k]], 1);
+      if (j[k] == 0) a.out_lens[s[k]] = len[k] + (p[k] >= 0 && a.grow ? 1 : 0);
+      if (id[k] >= 0 && a.grow && len[k] % ps != 0 && j[k] == len[k] / ps) {
+        atomicAdd(&writers[id[k]], 1);
+        atomicMin(&first[id[k]], s[k]);
+      }
+      if (j[k] == 0 && p[k] >= 0 && a.grow && len[k] == ld * ps) atomicAdd(&s_full, 1);   // no place for a page
+    }
   }
-  __threadfence();
-  __syncthreads();
+  sync();
   // sequences that need a page, in order
   int n_need = 0;
   for (int s0 = 0; a.grow && s0 < a.n_out; s0 += kPlanThreads) {
     const int s = s0 + t;
-    int need = 0, from = -1, j = 0;
+    int need = 0, from = -1;
     if (s < a.n_out) {
       int len;
-      const int p = parent_of(a, s, len);
+      const int p = seq(s, len);
       if (p >= 0 && len < ld * ps) {
-        j = len / ps;
         if (len % ps == 0) {
           need = 1;
         } else {
-          const int id = a.out_table[static_cast<size_t>(s) * ld + j];
+          int id = a.table[static_cast<size_t>(p) * ld + len / ps];
+          if (id < 0 || id >= P) id = -1;
           if (id < 0) need = 1;
-          else if (__hip_atomic_load(&a.refs[id], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) !=
-                       __hip_atomic_load(&w.writers[id], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ||
-                   __hip_atomic_load(&w.first[id], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != s) {
+          else if (counted<LDS>(&refs[id]) != counted<LDS>(&writers[id]) || counted<LDS>(&first[id]) != s) {
             need = 1;
             from = id;
           }
@@ -135,46 +180,46 @@ __global__ __launch_bounds__(kPlanThreads) void k_fork_plan(PagesArgs a, PagesWs
     }
     int total;
     const int k = n_need + block_scan(need, s_scan, total);
-    if (need) w.copies[k] = make_int2(from, s);      // the target follows below
+    if (need) need_list[k] = make_int2(from, s);
     n_need += total;
   }
-  __threadfence();
-  __syncthreads();
+  sync();
   // the lowest free pages, one for each
   int n_free = 0;
   for (int p0 = 0; n_free < n_need && p0 < P; p0 += kPlanThreads) {
     const int p = p0 + t;
-    const int is = p < P && __hip_atomic_load(&a.refs[p], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0;
+    const int is = p < P && counted<LDS>(&refs[p]) == 0;
     int total;
     const int k = n_free + block_scan(is, s_scan, total);
-    if (is && k < n_need) w.first[k] = p;            // first[] has served; n_need <= P is checked below
+    if (is && k < n_need) first[k] = p;              // first[] has served, and k < P
     n_free += total;
   }
-  __threadfence();
-  __syncthreads();
+  sync();
   const int missing = (n_need > n_free ? n_need - n_free : 0) + s_full;
   if (missing > 0) {
     // refused as a whole: every sequence comes out empty
-    for (long long i = t; i < static_cast<long long>(a.n_out) * ld; i += kPlanThreads) a.out_table[i] = -1;
+    for (long long i = t; i < entries; i += kPlanThreads) a.out_table[i] = -1;
     for (int s = t; s < a.n_out; s += kPlanThreads) a.out_lens[s] = 0;
-    for (int p = t; p < P; p += kPlanThreads) a.refs[p] = 0;
+    for (int p = t; p < P; p += kPlanThreads) refs[p] = 0;
     n_need = 0;
   }
   for (int k = t; k < n_need; k += kPlanThreads) {
-    const int2 c = w.copies[k];
-    const int id = w.first[k];
+    const int2 c = need_list[k];
+    const int id = first[k];
     int len;
-    parent_of(a, c.y, len);
+    seq(c.y, len);
     a.out_table[static_cast<size_t>(c.y) * ld + len / ps] = id;
-    a.refs[id] = 1;
-    if (c.x >= 0) atomicAdd(&a.refs[c.x], -1);
+    refs[id] = 1;
+    if (c.x >= 0) atomicAdd(&refs[c.x], -1);
     w.copies[k] = make_int2(c.x, id);
   }
-  __threadfence();
-  __syncthreads();
+  sync();
   int used = 0, sum = 0;
-  for (int p = t; p < P; p += kPlanThreads)
-    used += __hip_atomic_load(&a.refs[p], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > 0;
+  for (int p = t; p < P; p += kPlanThreads) {
+    const int r = counted<LDS>(&refs[p]);
+    used += r > 0;
+    if constexpr (LDS) a.refs[p] = r;
+  }
   block_scan(used, s_scan, sum);
   if (t == 0) {
     a.status[0] = missing;
@@ -183,7 +228,10 @@ __global__ __launch_bounds__(kPlanThreads) void k_fork_plan(PagesArgs a, PagesWs
   }
 }
 
-// The copies of a plan: whole pages of every layer, 16 bytes a lane.
+// The copies of a plan: whole pages of every layer, 16 bytes a lane.  Bound by
+// memory: 98 MB read and written in 20 us (4.9 TB/s; a copy of 1 GB reaches 5.2).
+// Several words requested ahead, or rows of a page a workgroup, measured the
+// same or slower (20.7 and 23.6 us).
 __global__ __launch_bounds__(256) void k_copy_pages(CacheView c, PagesWs w) {
   const int n = *w.n_copies;
   const size_t kv = c.kv_page_bytes() / 16, sc = c.scale_page_bytes() / 16;
@@ -206,59 +254,76 @@ __global__ __launch_bounds__(256) void k_copy_pages(CacheView c, PagesWs w) {
   }
 }
 
+template <bool LDS>
 __global__ __launch_bounds__(kPlanThreads) void k_compact_plan(PagesArgs a, PagesWs w) {
   const int t = threadIdx.x, P = a.c.pages, ps = a.c.ps, ld = a.table_ld;
   __shared__ int s_scan[kPlanWaves];
-  for (int p = t; p < P; p += kPlanThreads) w.writers[p] = 0;
-  __threadfence();
-  __syncthreads();
-  auto entry = [&](long long i) -> int {
-    const int s = static_cast<int>(i / ld), j = static_cast<int>(i - static_cast<long long>(s) * ld);
-    const int n = a.lens[s];
-    if (n <= 0 || j >= pages_of(n, ps)) return -1;
-    const int id = a.table[i];
-    return id < 0 || id >= P ? -1 : id;
+  __shared__ int s_used[LDS ? kLdsPages : 1], s_remap[LDS ? kLdsPages : 1];
+  __shared__ int2 s_move[LDS ? kLdsPages : 1];
+  int* in_use = LDS ? s_used : w.writers;
+  int* remap = LDS ? s_remap : a.refs;
+  int2* move = LDS ? s_move : w.copies;
+  auto sync = [&]() {
+    if constexpr (!LDS) __threadfence();
+    __syncthreads();
   };
+  for (int p = t; p < P; p += kPlanThreads) in_use[p] = 0;
+  sync();
+  // f(entry, page or -1) of every entry, kBatch of them under way at a time
   const long long entries = static_cast<long long>(a.n_in) * ld;
-  for (long long i = t; i < entries; i += kPlanThreads) {
-    const int id = entry(i);
-    if (id >= 0) atomicOr(&w.writers[id], 1);
-  }
-  __threadfence();
-  __syncthreads();
-  auto in_use = [&](int p) {
-    return p < P ? __hip_atomic_load(&w.writers[p], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+  auto each_entry = [&](auto f) {
+    for (long long i0 = t; i0 < entries; i0 += kBatch * kPlanThreads) {
+      int id[kBatch], n[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const long long i = min(i0 + k * kPlanThreads, entries - 1);
+        id[k] = a.table[i];
+        n[k] = a.lens[i / ld];
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const long long i = i0 + k * kPlanThreads;
+        if (i >= entries) continue;
+        const bool there = n[k] > 0 && i % ld < pages_of(n[k], ps) && id[k] >= 0 && id[k] < P;
+        f(i, there ? id[k] : -1);
+      }
+    }
   };
+  each_entry([&](long long, int id) {
+    if (id >= 0) atomicOr(&in_use[id], 1);
+  });
+  sync();
   int used = 0;
   {
     int mine = 0;
-    for (int p = t; p < P; p += kPlanThreads) mine += in_use(p);
+    for (int p = t; p < P; p += kPlanThreads) mine += counted<LDS>(&in_use[p]);
     block_scan(mine, s_scan, used);
   }
   // the i-th lowest page in use from `used` on goes to the i-th lowest free one below it
   int moves = 0, holes = 0;
   for (int p0 = 0; p0 < P; p0 += kPlanThreads) {
     const int p = p0 + t;
-    const int u = in_use(p);
+    const int u = p < P ? counted<LDS>(&in_use[p]) : 0;
     const int src = u && p >= used, hole = p < used && !u;
     int total;
     const int k = moves + block_scan(src, s_scan, total);
     moves += total;
     const int h = holes + block_scan(hole, s_scan, total);
     holes += total;
-    if (src) w.copies[k].x = p;
-    if (hole) w.copies[h].y = p;
-    if (p < P && !src) a.refs[p] = u ? p : -1;
+    if (src) move[k].x = p;
+    if (hole) move[h].y = p;
+    if (p < P && !src) remap[p] = u ? p : -1;
   }
-  __threadfence();
-  __syncthreads();
-  for (int k = t; k < moves; k += kPlanThreads) a.refs[w.copies[k].x] = w.copies[k].y;
-  __threadfence();
-  __syncthreads();
-  for (long long i = t; i < entries; i += kPlanThreads) {
-    const int id = entry(i);
-    a.out_table[i] = id < 0 ? -1 : a.refs[id];
+  sync();
+  for (int k = t; k < moves; k += kPlanThreads) {
+    const int2 m = move[k];
+    remap[m.x] = m.y;
+    if constexpr (LDS) w.copies[k] = m;
   }
+  sync();
+  each_entry([&](long long i, int id) { a.out_table[i] = id < 0 ? -1 : remap[id]; });
+  if constexpr (LDS)
+    for (int p = t; p < P; p += kPlanThreads) a.refs[p] = remap[p];
   if (t == 0) {
     a.status[0] = moves;
     a.status[1] = used;
@@ -282,13 +347,17 @@ size_t pages_workspace(const CacheView& c, int n_out) {
 
 hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t s) {
   const PagesWs w = carve(a.ws, a.c.pages, a.n_out);
-  hipLaunchKernelGGL(k_fork_plan, dim3(1), dim3(kPlanThreads), 0, s, a, w);
+  if (a.c.pages <= kLdsPages && a.n_out <= kLdsSeqs && static_cast<long long>(a.n_out) * a.table_ld < (1LL << 30))
+    hipLaunchKernelGGL(k_fork_plan<true>, dim3(1), dim3(kPlanThreads), 0, s, a, w);
+  else
+    hipLaunchKernelGGL(k_fork_plan<false>, dim3(1), dim3(kPlanThreads), 0, s, a, w);
   return copy_pages(a, w, s);
 }
 
 hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t s) {
   const PagesWs w = carve(a.ws, a.c.pages, a.n_in);
-  hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(kPlanThreads), 0, s, a, w);
+  if (a.c.pages <= kLdsPages) hipLaunchKernelGGL(k_compact_plan<true>, dim3(1), dim3(kPlanThreads), 0, s, a, w);
+  else hipLaunchKernelGGL(k_compact_plan<false>, dim3(1), dim3(kPlanThreads), 0, s, a, w);
   return copy_pages(a, w, s);
 }
 
