@@ -141,7 +141,7 @@ __device__ __forceinline__ void take_off(float* v, uint4 p) {   // v -= p
 // The eight codes of a word as bfloat16 16 + code: a code fills the top of the
 // mantissa of 16 (exact), two of them in a shift and an AND-OR (whose masks are
 // kept in vector registers: the instruction takes no two constants).  Scores
-// take the offset off with the least value; the product with V takes off
+// take the offset off with the least values; the product with V takes off
 // 16 + 7.5 inside the matrix product and adds the middle of a group's range
 // apart, because its sum over many keys of differing sign would otherwise be a
 // small difference of large numbers.
@@ -277,14 +277,14 @@ template <int N, typename F> __device__ __forceinline__ void each(F&& f) { each_
 // 16 t + 4 a + b), V rows by dimension, both padded so that the 16 rows of a read
 // start in different banks.  In 4 bits the (step, least) words of a row of
 // lanes' eight keys stay in registers, one a lane (word w = key * groups + group
-// in register w / 16 of lane w % 16).
+// in register w / 16 of lane w % 16); the keys' ones also lie behind their rows.
 template <int CT, int DH> struct Stage {
   static constexpr int NU = DH >= 32 ? DH / 32 : 1;
   static constexpr int NW = NU >= 2 ? NU / 2 : 1;
   static constexpr int kRow = CT == CT_F32 ? 4 * DH : CT == CT_BF16 ? 2 * DH : DH / 2;      // bytes of a key
   static constexpr int kSeg = CT == CT_F32 ? 128 : CT == CT_BF16 ? 64 : 16;                 // of 32 keys of a dimension
   static constexpr int kPiece = CT == CT_INT4 ? 8 : 16;
-  static constexpr int kRowLds = kRow >= 32 ? kRow + 16 : kRow;
+  static constexpr int kRowLds = kRow + 16;                                                 // 4 bits: a key's words behind it
   static constexpr int kSegLds = kSeg > 16 ? kSeg + 16 : kSeg;
   static constexpr int kOut = 16 * (DH + 4) * 4;                                            // of a wave's output
   static constexpr int kBytes = kBlock * kRowLds + DH * kSegLds > kOut ? kBlock * kRowLds + DH * kSegLds : kOut;
@@ -343,6 +343,14 @@ template <int CT, int DH> struct Stage {
     }
   }
   __device__ __forceinline__ void store(char* lds, int lane, int ps) const {
+    if constexpr (CT == CT_INT4) {
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const int at = 16 * w + (NU >= 2 ? lane & 15 : lane & 7), j = at / NU;
+        const int row = (j & 4) * 4 + (lane >> 4) * 4 + (j & 3);                            // of key 8 (lane / 16) + j
+        *reinterpret_cast<uint32_t*>(lds + row * kRowLds + kRow + 4 * (at % NU)) = kp[w];
+      }
+    }
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
       int x = i * kWave + lane;
@@ -459,13 +467,19 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
   const float s2 = a.scale * kLog2e;                  // scores come out in units of log 2
   uint4 qf[CT == CT_F32 ? 1 : NU][3];
   floatx4_t q32[NF];
-  float qsum[NU];                                     // 4 bits: sum of the row's queries over a group
+  uint4 qpar = make_uint4(0u, 0u, 0u, 0u);            // 4 bits: what multiplies a key's (step, least) words
   if constexpr (CT == CT_F32) {
 #pragma unroll
     for (int u = 0; u < NF; ++u)
 #pragma unroll
       for (int e = 0; e < 4; ++e) q32[u][e] = row_ok ? s2 * qv[u][e] : 0.f;
   } else {
+    // A score is sum_u step (sum_d (16 + code) q - 16 qs) + least qs with qs the
+    // sum of q over group u: the last two terms are a product of the key's words
+    // with (-16 qs, qs), a row of lanes for each bfloat16 part of those.
+    float par[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) par[e] = 0.f;
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
       float* v = qv[u];
@@ -475,11 +489,22 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
         v[e] = row_ok && (DH >= 32 || g < 2) ? s2 * v[e] : 0.f;
         sum += v[e];
       }
-      qsum[u] = xor32_sum(xor16_sum(sum));
+      if constexpr (CT == CT_INT4) {
+        par[2 * u + 1] = xor32_sum(xor16_sum(sum));
+        par[2 * u] = -16.f * par[2 * u + 1];
+      }
 #pragma unroll
       for (int part = 0; part < 3; ++part) {
         qf[u][part] = pack8(v);
         take_off(v, qf[u][part]);
+      }
+    }
+    if constexpr (CT == CT_INT4) {
+#pragma unroll
+      for (int part = 0; part < 3; ++part) {
+        const uint4 x = pack8(par);
+        if (g == part) qpar = x;
+        take_off(par, x);
       }
     }
   }
@@ -571,13 +596,10 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
       const bool whole = nv == kBlock && it.id0 >= 0 && it.id1 >= 0;
       // --- scores of keys 8 g + j, in units of log 2 ---
       constexpr int NW = SG::NW;
-      float sc[8], kstep[NW], kleast[NW];
+      float sc[8], kstep[NW];
       if constexpr (CT == CT_INT4) {
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-          kstep[w] = __uint_as_float(kp[w] << 16);
-          kleast[w] = fmaf(-16.f, kstep[w], __uint_as_float(kp[w] & 0xffff0000u));   // less the codes' offset
-        }
+        for (int w = 0; w < NW; ++w) kstep[w] = __uint_as_float(kp[w] << 16);
       }
       each<2>([&](auto t_) {
         constexpr int t = decltype(t_)::value;
@@ -597,6 +619,9 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
             for (int part = 0; part < 3; ++part) d = mma_bf16(x, qf[u][part], d);
           }
         } else {
+          const uint32_t* w4 = reinterpret_cast<const uint32_t*>(lds + (16 * t + n) * SG::kRowLds + SG::kRow);
+          d = mma_bf16(make_uint4(w4[0], NU > 1 ? w4[NU > 1 ? 1 : 0] : 0u, NU > 2 ? w4[NU > 2 ? 2 : 0] : 0u, NU > 2 ? w4[NU > 2 ? 3 : 0] : 0u),
+                       qpar, d);
           each<NU>([&](auto u_) {
             constexpr int u = decltype(u_)::value;
             floatx4_t x = {0.f, 0.f, 0.f, 0.f};
@@ -606,7 +631,6 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
             each<4>([&](auto i_) {
               constexpr int i2 = decltype(i_)::value, at = (4 * t + i2) * NU + u;
               d[i2] = fmaf(row_lane<at % 16>(kstep[at / 16]), x[i2], d[i2]);
-              d[i2] = fmaf(row_lane<at % 16>(kleast[at / 16]), qsum[u], d[i2]);
             });
           });
         }
@@ -615,6 +639,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
       });
       uint32_t live = 0xff;                             // keys of this lane that exist
       if (!whole) {
+        asm volatile("");                               // a branch: most items skip this
         const int here = (g < 2 ? it.id0 : it.id1) >= 0 ? max(0, min(8, nv - 8 * g)) : 0;
         live = (1u << here) - 1u;
 #pragma unroll
@@ -632,7 +657,11 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
         sum += p[j];
       }
       // --- weights times V ---
-      floatx4_t o[NT];
+      // 128 dimensions in 4 bits: a group's sums are taken over before the next
+      // group's are made (the registers of all of them do not fit two waves)
+      constexpr bool kByGroup = CT == CT_INT4 && DH >= 128;
+      constexpr int NG = NT / NU;
+      floatx4_t o[kByGroup ? NG : NT];
       float om[NU];
       if constexpr (CT == CT_F32) {
 #pragma unroll
@@ -693,24 +722,35 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
           const uint4 lo = pack8(r);
           floatx4_t base = mma_bf16(off, hi, floatx4_t{0.f, 0.f, 0.f, 0.f});
           base = mma_bf16(off, lo, base);
+          constexpr int o0 = kByGroup ? 0 : u * NG;
 #pragma unroll
-          for (int t = u * (NT / NU); t < (u + 1) * (NT / NU); ++t) {
-            const uint4 w = codes_bf16(*reinterpret_cast<const uint32_t*>(v_lds + t * 16 * SG::kSegLds), cm, ce);
-            o[t] = mma_bf16(w, hi, base);
-            o[t] = mma_bf16(w, lo, o[t]);
+          for (int t = 0; t < NG; ++t) {
+            const uint4 w = codes_bf16(*reinterpret_cast<const uint32_t*>(v_lds + (u * NG + t) * 16 * SG::kSegLds), cm, ce);
+            o[o0 + t] = mma_bf16(w, hi, base);
+            o[o0 + t] = mma_bf16(w, lo, o[o0 + t]);
+          }
+          if constexpr (kByGroup) {
+            if (own) {
+#pragma unroll
+              for (int t = 0; t < NG; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[u * NG + t][e] = fmaf(acc[u * NG + t][e], f, o[t][e]);
+            }
           }
         });
       }
       if (own) {
         l = fmaf(l, f, sum);
         m = mn;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[t][e] = fmaf(acc[t][e], f, o[t][e]);
         if constexpr (CT == CT_INT4) {
 #pragma unroll
           for (int u = 0; u < NU; ++u) mid[u] = fmaf(mid[u], f, om[u]);
+        }
+        if constexpr (!kByGroup) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[t][e] = fmaf(acc[t][e], f, o[t][e]);
         }
       }
     }
