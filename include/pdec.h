@@ -534,6 +534,37 @@ pd_status pd_pages_compact(const pd_cache* cache, const int32_t* table, int32_t 
                            int32_t n_seqs, int32_t* out_table, int32_t* out_remap, int32_t* out_status,
                            void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Beam search over the batch of the last pd_encode, on the operators above: per
+ * step a decoder forward of B * beam rows (self-attention over a paged cache
+ * whose pages the beams of a sentence share, cross-attention to the sentence's
+ * encoder memory), pd_beam_select and pd_pages_fork, captured as a graph.
+ *   beam        hypotheses per sentence, 1 .. 64 (1: greedy decoding)
+ *   alpha       length normalisation: hypotheses are ranked by
+ *               score / length^alpha (finite, >= 0)
+ *   cache_dtype storage of the self-attention cache: the model's dtype or PD_INT4
+ *   tgt_m       HOST int32 [B]: most tokens of a sentence's hypotheses
+ *               (1 .. max_tgt), [EOS] included; one that reaches it ends there
+ *   out_ids     device int32 [B][beam][out_ld], out_ld >= max(tgt_m): best
+ *               first, each with its [EOS] if it has one, [PAD]-filled
+ *   out_len     device int32 [B][beam] (0: no such hypothesis)
+ *   out_scores  device float [B][beam]: sums of log-probabilities (-inf: none)
+ *   out_k       device int32 [B]: decoder forwards that extended a hypothesis of
+ *               the sentence
+ *   out_flags   device int32 [B]: PD_FLAG_CONVERGED, PD_FLAG_EOS if the best
+ *               hypothesis ends in [EOS], PD_FLAG_NONFINITE
+ * A sentence ends when all its hypotheses have; finished ones stay in the beam
+ * and compete by their normalised score.  The workspace (256-byte aligned, at
+ * least pd_decode_beam_bytes) serves any batch of the context; it holds no
+ * state between calls, but steps are captured for its address, so it should be
+ * kept.  Like pd_decode, the call blocks the host until the search has ended
+ * and enqueues its outputs on the stream; it uses the context's workspace too.
+ */
+pd_status pd_decode_beam_bytes(const pd_ctx* ctx, int32_t beam, int32_t cache_dtype, size_t* bytes);
+pd_status pd_decode_beam(pd_ctx* ctx, int32_t beam, float alpha, int32_t cache_dtype, const int32_t* tgt_m,
+                         int32_t* out_ids, int32_t out_ld, int32_t* out_len, float* out_scores, int32_t* out_k,
+                         int32_t* out_flags, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char* pd_last_error(void);
 

@@ -18,7 +18,7 @@ LIB = os.path.join(HERE, "libpdec.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["gemm.hip", "gemm_feed.hip", "gemm_stage.hip", "vocab.hip", "decode_kernels.hip", "static_scratch.hip",
-           "beam_select.hip", "cache_attn.hip", "pages.hip", "operators.cpp", "runtime.cpp"]
+           "beam_select.hip", "cache_attn.hip", "pages.hip", "beam_path.hip", "operators.cpp", "runtime.cpp"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", "-Wno-unused-result"]
 DEVICE = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

@@ -472,6 +472,11 @@ size_t select_workspace(int dtype, int B, int beam, int vocab) {
   return units * (static_cast<size_t>(beam) * sizeof(u64) + sizeof(PartStat));
 }
 
+// parts <= (kWantWaves + rows - 1) / rows, so rows * parts < kWantWaves + rows.
+size_t select_workspace_most(int rows, int beam) {
+  return (static_cast<size_t>(rows) + kWantWaves) * (static_cast<size_t>(beam) * sizeof(u64) + sizeof(PartStat));
+}
+
 hipError_t launch_beam_select(const SelectArgs& a, hipStream_t s) {
   const int rows = a.B * a.beam;
   const Split sp = split_rows(a.dtype, rows, a.vocab);

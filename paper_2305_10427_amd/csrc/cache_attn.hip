@@ -926,6 +926,10 @@ size_t attend_workspace(const CacheView& c, int n_seqs, int heads, int group, in
   return p.splits == 1 ? 0 : static_cast<size_t>(p.splits) * n_seqs * heads * (c.dh * 4 + 8);
 }
 
+// Parts are made up to kCus * waves_per_simd (at most 4 kCus) workgroups of at
+// most 16 rows.
+size_t attend_workspace_most(const CacheView& c) { return static_cast<size_t>(4 * kCus) * 16 * (c.dh * 4 + 8); }
+
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t s) {
   const Plan p = plan_attend(a.c, a.n_seqs, a.heads, a.group, a.max_len);
   if (a.c.type == CT_F32) return launch_attend_ct<CT_F32>(a, p, s);

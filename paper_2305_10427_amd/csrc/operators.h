@@ -50,6 +50,7 @@ struct SelectArgs {
   char* ws;
 };
 size_t select_workspace(int dtype, int B, int beam, int vocab);
+size_t select_workspace_most(int rows, int beam);      // of any launch of up to so many rows
 hipError_t launch_beam_select(const SelectArgs& a, hipStream_t s);
 
 struct AttendArgs {
@@ -74,6 +75,7 @@ struct AttendArgs {
   char* ws;
 };
 size_t attend_workspace(const CacheView& c, int n_seqs, int heads, int group, int max_len);
+size_t attend_workspace_most(const CacheView& c);      // of any launch on such a cache
 hipError_t launch_cache_attend(const AttendArgs& a, hipStream_t s);
 
 struct ReadArgs {
@@ -107,5 +109,27 @@ struct PagesArgs {
 size_t pages_workspace(const CacheView& c, int n_out);
 hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t s);
 hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t s);
+
+// State of a beam decode (device arrays of R = B * beam rows unless noted).
+struct BeamArgs {
+  int B, beam, steps_max;
+  float* scores;
+  int *lens, *done, *parent, *token, *src;
+  int* cache_lens;             // lengths of the first page table
+  int *row_sent, *row_pos, *row_tok;
+  int *k, *flags, *step_flags, *finished;   // [B]
+  int2* hist;                  // [steps_max][R] (parent, token)
+  int* step;                   // device scalar: steps done
+  int* seq;                    // the context's control-step counter and host word, as CtrlArgs'
+  int seq0;
+  int* host_rows;
+  int pad_id, bos_id, eos_id, flag_converged, flag_eos;
+  int *out_ids, *out_len, *out_k, *out_flags;
+  float* out_scores;
+  int out_ld;
+};
+hipError_t launch_beam_init(const BeamArgs& a, hipStream_t s);
+hipError_t launch_beam_step(const BeamArgs& a, hipStream_t s);
+hipError_t launch_beam_out(const BeamArgs& a, hipStream_t s);
 
 }  // namespace pdec

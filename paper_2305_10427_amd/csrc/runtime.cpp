@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "operators.h"
 #include "../../include/pdec.h"
 
 using namespace pdec;
@@ -222,11 +223,28 @@ struct IterGraph {
   int64_t kernels;                     // kernel nodes of the captured iteration
 };
 
+// A captured step of beam decoding; every buffer of it lies in the workspace.
+struct BeamKey {
+  int B, beam, cache, attn_len, long_src, parity;
+  float alpha;
+  const void* ws;
+  bool operator==(const BeamKey& o) const {
+    return B == o.B && beam == o.beam && cache == o.cache && attn_len == o.attn_len && long_src == o.long_src &&
+           parity == o.parity && alpha == o.alpha && ws == o.ws;
+  }
+};
+
+struct BeamGraph {
+  BeamKey key;
+  hipGraphExec_t exec;
+};
+
 struct pd_ctx {
   const pd_model* M;
   hipStream_t capture = nullptr;       // private stream used only to capture iteration graphs
   bool use_graphs = true;
   std::vector<IterGraph> graphs;
+  std::vector<BeamGraph> beam_graphs;
   int64_t iter_kernels = 0;            // kernels of the iteration graph replayed last
   int max_batch, max_src, max_tgt;
   char* ws;
@@ -373,16 +391,26 @@ hipError_t embed_rows(pd_ctx& C, const Rows& r, hipStream_t s) {
   return launch_embed(M.dt, ea, r.R_max, s);
 }
 
-hipError_t decoder_pass(pd_ctx& C, const Rows& r, float* logits, hipStream_t s, int slot = -1, bool fused = false) {
+// A step of beam decoding: its own activation buffers (a context's are sized for
+// max_batch * max_tgt rows, not for the beams), the rows' embedding already made,
+// and self-attention over a paged cache, to which a layer's keys and values go
+// from new_k / new_v (att: everything but the layer).
+struct BeamPass {
+  char *x_res, *s_buf, *q_buf, *a_buf, *h_buf, *new_k, *new_v;
+  AttendArgs att;
+};
+
+hipError_t decoder_pass(pd_ctx& C, const Rows& r, float* logits, hipStream_t s, int slot = -1, bool fused = false,
+                        const BeamPass* bp = nullptr) {
   const pd_model& M = *C.M;
   const pd_config& cfg = M.cfg;
   const int d = M.d;
   const bool pre = cfg.pre_ln != 0;
-  void* x_res = C.at<char>(C.L.x_res);
-  float* s_buf = C.at<float>(C.L.s_buf);
-  float* q_buf = C.at<float>(C.L.q_buf);
-  void* a_buf = C.at<char>(C.L.a_buf);
-  void* h_buf = C.at<char>(C.L.h_buf);
+  void* x_res = bp ? bp->x_res : C.at<char>(C.L.x_res);
+  float* s_buf = bp ? reinterpret_cast<float*>(bp->s_buf) : C.at<float>(C.L.s_buf);
+  float* q_buf = bp ? reinterpret_cast<float*>(bp->q_buf) : C.at<float>(C.L.q_buf);
+  void* a_buf = bp ? bp->a_buf : C.at<char>(C.L.a_buf);
+  void* h_buf = bp ? bp->h_buf : C.at<char>(C.L.h_buf);
   const size_t es = M.dt == DT_BF16 ? 2 : 4;
   const size_t self_layer = static_cast<size_t>(C.max_batch) * C.max_tgt * d * es;
   const size_t cross_layer = static_cast<size_t>(C.max_batch) * C.max_src * d * es;
@@ -420,17 +448,28 @@ hipError_t decoder_pass(pd_ctx& C, const Rows& r, float* logits, hipStream_t s, 
     g.out_f32 = q_buf; g.ldo = d; g.q_cols = d;
     g.kc = C.at<char>(C.L.self_k) + l * self_layer; g.vc = C.at<char>(C.L.self_v) + l * self_layer;
     g.H = M.H; g.dh = M.dh; g.T = C.max_tgt; g.d = d;
+    if (bp != nullptr) {   // K/V as one row a sequence, [rows][d]
+      g.kc = bp->new_k; g.vc = bp->new_v; g.T = 1;
+      g.rows = RowMap{nullptr, nullptr, 1};
+    }
     if ((e = run_gemm(C, r, g, EPI_QKV, ln_qkv, a_buf, s)) != hipSuccess) return e;
 
-    AttnArgs aa{r.n_dev, r.n_host, q_buf, d, g.kc, g.vc, M.H, M.dh, C.max_tgt, r.map, 1, nullptr,
-                a_buf, d, 1.0f / std::sqrt(static_cast<float>(M.dh))};
-    aa.out_feed = feed;
-    aa.max_keys = C.self_keys;
-    aa.sent_rows = C.sent_rows; aa.st = C.at<SentState>(C.L.st); aa.n_sent = C.enc_B;
-    if ((e = launch_attn(M.dt, aa, r.R_max, s)) != hipSuccess) return e;
+    AttnArgs aa;
+    if (bp != nullptr) {
+      AttendArgs at = bp->att;
+      at.layer = l;
+      if ((e = launch_cache_attend(at, s)) != hipSuccess) return e;
+    } else {
+      aa = AttnArgs{r.n_dev, r.n_host, q_buf, d, g.kc, g.vc, M.H, M.dh, C.max_tgt, r.map, 1, nullptr,
+                    a_buf, d, 1.0f / std::sqrt(static_cast<float>(M.dh))};
+      aa.out_feed = feed;
+      aa.max_keys = C.self_keys;
+      aa.sent_rows = C.sent_rows; aa.st = C.at<SentState>(C.L.st); aa.n_sent = C.enc_B;
+      if ((e = launch_attn(M.dt, aa, r.R_max, s)) != hipSuccess) return e;
+    }
 
     g = gemm_base(r);
-    g.x = a_buf; g.ldx = d; g.x_feed = feed;
+    g.x = a_buf; g.ldx = d; g.x_feed = bp != nullptr ? 0 : feed;   // the cache's attention writes row-major
     g.w = M.dec(l, D_WO); g.wp = M.dec_feed(l, D_WO); g.bias = M.dec(l, D_BO); g.N = d; g.K = d;
     g.resid = x_res; g.ldr = d; g.ldo = d;
     if (pre) g.out = x_res; else g.out_f32 = s_buf;
@@ -668,22 +707,30 @@ hipError_t iteration(pd_ctx& C, const Rows& r, const CtrlArgs& ca, hipStream_t s
   return launch_ctrl_step(C.M->dt, ca, s);
 }
 
-// The iteration as a HIP graph, captured once per context and launch shape.
-hipError_t iteration_graph(pd_ctx& C, const GraphKey& key, const Rows& r, const CtrlArgs& ca, hipGraphExec_t* out) {
-  for (auto& ig : C.graphs)
-    if (ig.key == key) { *out = ig.exec; C.iter_kernels = ig.kernels; return hipSuccess; }
+// What body launches, captured on the context's private stream.
+template <typename Body>
+hipError_t capture_graph(pd_ctx& C, Body body, hipGraphExec_t* out, size_t* nodes) {
   hipError_t e = hipStreamBeginCapture(C.capture, hipStreamCaptureModeThreadLocal);
   if (e != hipSuccess) return e;
-  hipError_t e_body = iteration(C, r, ca, C.capture, key.slot, key.fused != 0);
+  const hipError_t e_body = body(C.capture);
   hipGraph_t g = nullptr;
   e = hipStreamEndCapture(C.capture, &g);
   if (e_body != hipSuccess) { if (g) hipGraphDestroy(g); return e_body; }
   if (e != hipSuccess) return e;
-  size_t nodes = 0;
-  e = hipGraphGetNodes(g, nullptr, &nodes);
-  hipGraphExec_t ex = nullptr;
-  if (e == hipSuccess) e = hipGraphInstantiate(&ex, g, nullptr, nullptr, 0);
+  if (nodes != nullptr) e = hipGraphGetNodes(g, nullptr, nodes);
+  if (e == hipSuccess) e = hipGraphInstantiate(out, g, nullptr, nullptr, 0);
   hipGraphDestroy(g);
+  return e;
+}
+
+// The iteration as a HIP graph, captured once per context and launch shape.
+hipError_t iteration_graph(pd_ctx& C, const GraphKey& key, const Rows& r, const CtrlArgs& ca, hipGraphExec_t* out) {
+  for (auto& ig : C.graphs)
+    if (ig.key == key) { *out = ig.exec; C.iter_kernels = ig.kernels; return hipSuccess; }
+  size_t nodes = 0;
+  hipGraphExec_t ex = nullptr;
+  const hipError_t e = capture_graph(
+      C, [&](hipStream_t cs) { return iteration(C, r, ca, cs, key.slot, key.fused != 0); }, &ex, &nodes);
   if (e != hipSuccess) return e;
   C.graphs.push_back(IterGraph{key, ex, static_cast<int64_t>(nodes)});
   C.iter_kernels = static_cast<int64_t>(nodes);
@@ -756,6 +803,112 @@ hipError_t take_timing(pd_ctx& C, int slot) {
   C.tv_launches += 1;
   C.tv_pending[slot] = false;
   return hipSuccess;
+}
+
+// --- beam decoding ---
+
+constexpr int kBeamPage = 16;     // tokens per page: a copy of a half-filled page moves at most 15 of others' tokens
+
+// Workspace of a beam decode: activations of the rows, the page pool with every
+// page that max_batch * beam hypotheses of max_tgt tokens can need, two page
+// tables (a step reads one and fills the other) and the search's state.
+struct BeamLayout {
+  size_t x_res, s_buf, q_buf, a_buf, h_buf, new_k, new_v, logits;
+  size_t k, v, ks, vs, table[2], lens[2], refs, status;
+  size_t scores, hlen, done, parent, token, src, flags, step_flags, finished, n_fwd, row_sent, row_pos, row_tok, hist, step;
+  size_t select_ws, attend_ws, pages_ws, total;
+  CacheView cache;
+  int ld;
+};
+
+BeamLayout beam_plan(const pd_ctx& C, int beam, int cache_type) {
+  const pd_model& M = *C.M;
+  BeamLayout L{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += (bytes + kAlign - 1) / kAlign * kAlign;
+    return at;
+  };
+  const size_t es = M.dt == DT_BF16 ? 2 : 4, d = M.d;
+  const size_t R = static_cast<size_t>(C.max_batch) * beam, R16 = (R + 15) / 16 * 16;
+  L.ld = (C.max_tgt + kBeamPage - 1) / kBeamPage;
+  CacheView& c = L.cache;
+  c = CacheView{cache_type, M.cfg.n_dec, static_cast<int>(R) * L.ld, kBeamPage, M.H, M.dh, M.dh > 32 ? M.dh / 32 : 1,
+                nullptr, nullptr, nullptr, nullptr};
+  const size_t pages = static_cast<size_t>(c.layers) * c.pages;
+  L.x_res = take(R * d * es);
+  L.s_buf = take(R * d * 4);
+  L.q_buf = take(R * d * 4);
+  L.a_buf = take(R16 * d * es);
+  L.h_buf = take(R16 * M.dff * es);
+  L.new_k = take(R * d * es);
+  L.new_v = take(R * d * es);
+  L.logits = take(R * M.V * 4);
+  L.k = take(pages * c.kv_page_bytes());
+  L.v = take(pages * c.kv_page_bytes());
+  L.ks = take(pages * c.scale_page_bytes());
+  L.vs = take(pages * c.scale_page_bytes());
+  for (int i = 0; i < 2; ++i) {
+    L.table[i] = take(R * L.ld * 4);
+    L.lens[i] = take(R * 4);
+  }
+  L.refs = take(static_cast<size_t>(c.pages) * 4);
+  L.status = take(8);
+  for (size_t* p : {&L.scores, &L.hlen, &L.done, &L.parent, &L.token, &L.src, &L.row_sent, &L.row_pos, &L.row_tok}) *p = take(R * 4);
+  for (size_t* p : {&L.flags, &L.step_flags, &L.finished, &L.n_fwd}) *p = take(static_cast<size_t>(C.max_batch) * 4);
+  L.hist = take(static_cast<size_t>(C.max_tgt) * R * sizeof(int2));
+  L.step = take(4);
+  L.select_ws = take(select_workspace_most(static_cast<int>(R), beam));
+  L.attend_ws = take(attend_workspace_most(c));
+  L.pages_ws = take(pages_workspace(c, static_cast<int>(R)));
+  L.total = off;
+  return L;
+}
+
+pd_status check_beam(const pd_ctx* ctx, int32_t beam, int32_t cache_dtype) {
+  if (ctx == nullptr) return fail(PD_E_ARG, "null context");
+  if (beam < 1) return fail(PD_E_ARG, "beam must be >= 1");
+  if (beam > kMaxBeam) return fail(PD_E_SHAPE, "at most 64 beams");
+  if (cache_dtype != ctx->M->cfg.dtype && cache_dtype != PD_INT4)
+    return fail(PD_E_ARG, "cache_dtype must be the model's dtype or PD_INT4");
+  const long long R = static_cast<long long>(ctx->max_batch) * beam;
+  const long long ld = (ctx->max_tgt + kBeamPage - 1) / kBeamPage;
+  if (R * ctx->M->H > (1LL << 22) || R * ld > (1LL << 24))
+    return fail(PD_E_SHAPE, "max_batch * beam is too large: at most 2^22 rows times heads and 2^24 pages");
+  return PD_OK;
+}
+
+// One step: the cache follows the survivors, a decoder pass over the rows, the
+// selection and the book-keeping.
+hipError_t beam_step(pd_ctx& C, const BeamLayout& L, char* ws, int beam, float alpha, int attn_len, int parity,
+                     const BeamArgs& ba, hipStream_t s) {
+  const pd_model& M = *C.M;
+  const int B = C.enc_B, R = B * beam;
+  auto at = [&](size_t off) { return ws + off; };
+  auto ints = [&](size_t off) { return reinterpret_cast<int*>(ws + off); };
+  CacheView c = L.cache;
+  c.k = at(L.k); c.v = at(L.v); c.ks = at(L.ks); c.vs = at(L.vs);
+  int* table = ints(L.table[1 - parity]);
+  int* lens = ints(L.lens[1 - parity]);
+  const PagesArgs pa{c, ints(L.table[parity]), L.ld, ints(L.lens[parity]), R, ints(L.src), R, 1, table, lens,
+                     ints(L.refs), ints(L.status), at(L.pages_ws)};
+  hipError_t e = launch_pages_fork(pa, s);
+  if (e != hipSuccess) return e;
+  const Rows r{nullptr, R, RowMap{nullptr, nullptr, beam}, ints(L.row_tok), R};
+  EmbedArgs ea{nullptr, R, r.tok, RowMap{ints(L.row_sent), ints(L.row_pos), 0}, M.w[0], C.at<float>(C.L.pe), M.dec_scale,
+               M.d, M.V, at(L.x_res)};
+  if ((e = launch_embed(M.dt, ea, R, s)) != hipSuccess) return e;
+  const int bf16 = M.dt == DT_BF16 ? 1 : 0;
+  BeamPass bp{at(L.x_res), at(L.s_buf), at(L.q_buf), at(L.a_buf), at(L.h_buf), at(L.new_k), at(L.new_v), AttendArgs{}};
+  bp.att = AttendArgs{c, 0, at(L.q_buf), 0, M.d, M.H, at(L.new_k), at(L.new_v), bf16, M.d, table, L.ld, lens, R, beam, attn_len,
+                      1.0f / std::sqrt(static_cast<float>(M.dh)), at(L.a_buf), bf16, M.d, at(L.attend_ws)};
+  if ((e = decoder_pass(C, r, reinterpret_cast<float*>(at(L.logits)), s, -1, true, &bp)) != hipSuccess) return e;
+  const SelectArgs sa{at(L.logits), DT_F32, M.V, B, beam, M.V, ba.scores, ba.lens, ba.done, C.at<int>(C.L.tgt_m),
+                      M.cfg.eos_id, M.cfg.pad_id, alpha, ba.scores, ba.parent, ba.token, ba.lens, ba.done, ba.src,
+                      ba.step_flags, at(L.select_ws)};
+  if ((e = launch_beam_select(sa, s)) != hipSuccess) return e;
+  return launch_beam_step(ba, s);
 }
 
 }  // namespace
@@ -927,6 +1080,7 @@ void pd_ctx_destroy(pd_ctx* ctx) {
     for (auto ev : ctx->pg0[i]) hipEventDestroy(ev);
   }
   for (auto& ig : ctx->graphs) hipGraphExecDestroy(ig.exec);
+  for (auto& bg : ctx->beam_graphs) hipGraphExecDestroy(bg.exec);
   if (ctx->capture) hipStreamDestroy(ctx->capture);
   hipHostFree(ctx->host_pinned);
   delete ctx;
@@ -1114,6 +1268,113 @@ pd_status pd_decode_init(pd_ctx* ctx, int32_t mode, int32_t block, int32_t horiz
     for (int slot = 0; slot < 2; ++slot)
       if ((e = take_timing(C, slot)) != hipSuccess) return fail(PD_E_DEVICE, std::string("timing: ") + hipGetErrorString(e));
   }
+  return PD_OK;
+}
+
+pd_status pd_decode_beam_bytes(const pd_ctx* ctx, int32_t beam, int32_t cache_dtype, size_t* bytes) {
+  if (bytes == nullptr) return fail(PD_E_ARG, "null argument");
+  const pd_status st = check_beam(ctx, beam, cache_dtype);
+  if (st != PD_OK) return st;
+  *bytes = beam_plan(*ctx, beam, cache_dtype).total;
+  return PD_OK;
+}
+
+pd_status pd_decode_beam(pd_ctx* ctx, int32_t beam, float alpha, int32_t cache_dtype, const int32_t* tgt_m,
+                         int32_t* out_ids, int32_t out_ld, int32_t* out_len, float* out_scores, int32_t* out_k,
+                         int32_t* out_flags, void* workspace, size_t workspace_bytes, void* stream) {
+  pd_status st = check_beam(ctx, beam, cache_dtype);
+  if (st != PD_OK) return st;
+  if (tgt_m == nullptr || out_ids == nullptr || out_len == nullptr || out_scores == nullptr || out_k == nullptr ||
+      out_flags == nullptr)
+    return fail(PD_E_ARG, "null argument");
+  if (!(alpha >= 0.f) || !std::isfinite(alpha)) return fail(PD_E_ARG, "alpha must be finite and >= 0");
+  if (!ctx->encoded) return fail(PD_E_STATE, "pd_decode_beam called before pd_encode");
+  pd_ctx& C = *ctx;
+  const int B = C.enc_B;
+  int m_max = 0;
+  for (int b = 0; b < B; ++b) {
+    if (tgt_m[b] < 1 || tgt_m[b] > C.max_tgt) return fail(PD_E_SHAPE, "tgt_m[" + std::to_string(b) + "] out of [1, max_tgt]");
+    m_max = std::max(m_max, tgt_m[b]);
+  }
+  if (out_ld < m_max) return fail(PD_E_ARG, "out_ld must be >= max(tgt_m)");
+  const BeamLayout L = beam_plan(C, beam, cache_dtype);
+  if (workspace == nullptr || !aligned(workspace, kAlign))
+    return fail(PD_E_WORKSPACE, "workspace is null or not 256-byte aligned");
+  if (workspace_bytes < L.total)
+    return fail(PD_E_WORKSPACE, "workspace too small: need " + std::to_string(L.total) + " bytes");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  if ((st = stage_lengths(ctx, C.stage_tgt, tgt_m, B, C.at<int>(C.L.tgt_m), s)) != PD_OK) return st;
+  C.sent_rows = beam;
+  auto ints = [&](size_t off) { return reinterpret_cast<int*>(ws + off); };
+  BeamArgs ba;
+  std::memset(&ba, 0, sizeof(ba));
+  ba.B = B;
+  ba.beam = beam;
+  ba.steps_max = C.max_tgt;
+  ba.scores = reinterpret_cast<float*>(ws + L.scores);
+  ba.lens = ints(L.hlen);
+  ba.done = ints(L.done);
+  ba.parent = ints(L.parent);
+  ba.token = ints(L.token);
+  ba.src = ints(L.src);
+  ba.cache_lens = ints(L.lens[0]);
+  ba.row_sent = ints(L.row_sent);
+  ba.row_pos = ints(L.row_pos);
+  ba.row_tok = ints(L.row_tok);
+  ba.k = ints(L.n_fwd);
+  ba.flags = ints(L.flags);
+  ba.step_flags = ints(L.step_flags);
+  ba.finished = ints(L.finished);
+  ba.hist = reinterpret_cast<int2*>(ws + L.hist);
+  ba.step = ints(L.step);
+  ba.seq = C.at<int>(C.L.seq);
+  ba.host_rows = C.host_rows_dev;
+  ba.pad_id = C.M->cfg.pad_id;
+  ba.bos_id = C.M->cfg.bos_id;
+  ba.eos_id = C.M->cfg.eos_id;
+  ba.flag_converged = PD_FLAG_CONVERGED;
+  ba.flag_eos = PD_FLAG_EOS;
+  BeamArgs b0 = ba;                  // what only the first and last launches read stays out of the captured steps
+  b0.seq0 = C.seq_next;
+  hipError_t e = launch_beam_init(b0, s);
+  if (e != hipSuccess) return fail(PD_E_DEVICE, std::string("init launch: ") + hipGetErrorString(e));
+  C.seq_next = (C.seq_next + 1) & kSeqMask;
+  const int attn_len = (m_max + 127) / 128 * 128;    // the attention's launch choice only
+  for (int it = 0; it < m_max; ++it) {
+    const int parity = it & 1;
+    if (C.use_graphs) {
+      const BeamKey key{B, beam, cache_dtype, attn_len, C.src_keys > kAttnChunkKeys ? 1 : 0, parity, alpha, ws};
+      hipGraphExec_t ex = nullptr;
+      for (auto& bg : C.beam_graphs)
+        if (bg.key == key) ex = bg.exec;
+      if (ex == nullptr) {
+        e = capture_graph(C, [&](hipStream_t cs) { return beam_step(C, L, ws, beam, alpha, attn_len, parity, ba, cs); }, &ex, nullptr);
+        if (e == hipSuccess) C.beam_graphs.push_back(BeamGraph{key, ex});
+      }
+      if (e == hipSuccess) e = hipGraphLaunch(ex, s);
+    } else {
+      e = beam_step(C, L, ws, beam, alpha, attn_len, parity, ba, s);
+    }
+    if (e != hipSuccess) return fail(PD_E_DEVICE, std::string("beam step launch: ") + hipGetErrorString(e));
+    const int q = C.seq_next;
+    C.seq_next = (C.seq_next + 1) & kSeqMask;
+    if (it >= 1) {   // the step before this one says how many hypotheses still grow; the next is queued behind it
+      int word = 0;
+      if ((e = wait_word(C.host_pinned, q - 1, s, &word)) != hipSuccess)
+        return fail(PD_E_DEVICE, std::string("beam step: ") + hipGetErrorString(e));
+      if ((word & kRowsMask) == 0) break;
+    }
+  }
+  ba.out_ids = out_ids;
+  ba.out_ld = out_ld;
+  ba.out_len = out_len;
+  ba.out_scores = out_scores;
+  ba.out_k = out_k;
+  ba.out_flags = out_flags;
+  e = launch_beam_out(ba, s);
+  if (e == hipSuccess) e = hipEventRecord(C.it_ev[0], s);
+  if (e != hipSuccess) return fail(PD_E_DEVICE, std::string("beam output launch: ") + hipGetErrorString(e));
   return PD_OK;
 }
 

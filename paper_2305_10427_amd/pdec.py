@@ -52,7 +52,7 @@ EXPORTS = ("pd_weight_count", "pd_weight_shape", "pd_model_create", "pd_model_de
            "pd_trace_scratch_bytes", "pd_ctx_set_trace", "pd_ctx_trace_count", "pd_ctx_product_timing",
            "pd_ctx_iteration_kernels", "pd_decode_traced_static", "pd_beam_select_bytes", "pd_beam_select",
            "pd_cache_bytes", "pd_cache_attend_bytes", "pd_cache_attend", "pd_cache_read", "pd_pages_bytes",
-           "pd_pages_fork", "pd_pages_compact", "pd_last_error")
+           "pd_pages_fork", "pd_pages_compact", "pd_decode_beam_bytes", "pd_decode_beam", "pd_last_error")
 TRACE_STATIC_BYTES = 8 << 20      # PD_TRACE_STATIC_BYTES
 
 CACHE_TYPES = {"f32": 0, "bf16": 1, "int4": 2}      # PD_F32, PD_BF16, PD_INT4
@@ -138,6 +138,10 @@ def load_library(path: str = LIB_PATH):
     L.pd_pages_fork.restype = I32
     L.pd_pages_compact.argtypes = [PC, VP, I32, VP, I32, VP, VP, VP, VP, SZ, VP]
     L.pd_pages_compact.restype = I32
+    L.pd_decode_beam_bytes.argtypes = [VP, I32, I32, P(SZ)]
+    L.pd_decode_beam_bytes.restype = I32
+    L.pd_decode_beam.argtypes = [VP, I32, F32, I32, P(I32), VP, I32, VP, VP, VP, VP, VP, SZ, VP]
+    L.pd_decode_beam.restype = I32
     L.pd_last_error.argtypes = []
     L.pd_last_error.restype = ctypes.c_char_p
     _lib = L
@@ -224,6 +228,7 @@ class Context:
         self.handle = h
         self.B = 0
         self.device = device
+        self._beam_ws = {}
 
     def encode(self, src, src_len: Sequence[int], stream=None):
         """src: int32 device tensor [B, n_max]; src_len: host ints."""
@@ -270,6 +275,35 @@ class Context:
                                                  ctypes.c_void_p(fl.data_ptr()),
                                                  ctypes.c_void_p(_stream_handle(stream))))
         return ids, ln, k, fl
+
+    def decode_beam(self, tgt_m: Sequence[int], beam: int = 5, alpha: float = 1.0, cache: str = "native", stream=None):
+        """Beam search (pd_decode_beam): (ids [B, beam, m_max], lengths [B, beam], scores [B, beam] float32, k [B],
+        flags [B]) as device tensors, hypotheses best first.  cache: "native" (the model's type) or "int4".  The
+        workspace of a beam width and cache type is kept with the context."""
+        import torch
+        tgt_m = [int(x) for x in tgt_m]
+        if len(tgt_m) != self.B:
+            raise PdError(1, f"tgt_m has {len(tgt_m)} entries, the encoded batch has {self.B}")
+        if cache not in ("native", "int4"):
+            raise PdError(1, f"unknown cache type {cache!r}")
+        L = load_library()
+        dt = CACHE_TYPES[self.model.cfg.dtype if cache == "native" else cache]
+        key = (int(beam), dt)
+        if key not in self._beam_ws:
+            n = ctypes.c_size_t()
+            _check(L.pd_decode_beam_bytes(self.handle, int(beam), dt, ctypes.byref(n)))
+            self._beam_ws[key] = torch.empty(n.value + 256, dtype=torch.uint8, device=self.device), n.value
+        ws, need = self._beam_ws[key]
+        B, m_max = len(tgt_m), max(tgt_m, default=0)
+        rows = max(B, 1)                     # nothing encoded: the library itself reports it
+        ids = torch.empty((rows, beam, max(m_max, 1)), dtype=torch.int32, device=self.device)
+        ln = torch.empty((rows, beam), dtype=torch.int32, device=self.device)
+        scores = torch.empty((rows, beam), dtype=torch.float32, device=self.device)
+        k, fl = (torch.empty(rows, dtype=torch.int32, device=self.device) for _ in range(2))
+        _check(L.pd_decode_beam(self.handle, int(beam), float(alpha), dt, _host_i32(tgt_m), ids.data_ptr(), ids.shape[2],
+                                ln.data_ptr(), scores.data_ptr(), k.data_ptr(), fl.data_ptr(),
+                                (ws.data_ptr() + 255) // 256 * 256, need, _stream_handle(stream)))
+        return ids, ln, scores, k, fl
 
     def decode_traced_static(self, mode, tgt_m: Sequence[int], capacity: int, block: int = 1, max_iters: int = 0,
                              horizon: int = 0, stream=None, stop: str = "block"):
