@@ -882,10 +882,12 @@ namespace {
 // Beams per tile: whole beams within 16 query rows.  Parts of the keys: as many
 // as the chip holds workgroups at once, a second round of workgroups costing
 // more than it evens out (64 x 4 rows of 4,000 keys, 64 wide: bfloat16 73 us with
-// 768 workgroups, 103 with 1,024; 4 bits 55 and 71), while a part has at least
-// kMinUnits units.
+// 768 workgroups, 103 with 1,024; 4 bits 55 and 71); but one below kSplitUnits
+// units, where joining the parts costs more than the workgroup's longer way (5
+// rows of 8 heads, bfloat16, one part / parts of a unit and their join: 138 keys
+// 9.5 / 11.6 us, 300 12.2 / 12.7, 600 17.1 / 14.0, 1,024 24.5 / 14.9).
 constexpr int kCus = 256;
-constexpr int kMinUnits = 1;
+constexpr int kSplitUnits = 4;
 Plan plan_attend(const CacheView& c, int n_seqs, int heads, int group, int max_len) {
   Plan p;
   const int G = heads / c.kv_heads;
@@ -893,9 +895,9 @@ Plan plan_attend(const CacheView& c, int n_seqs, int heads, int group, int max_l
   p.tiles = (group + p.rows_per_tile - 1) / p.rows_per_tile;
   const int units = (max_len + kUnit * kBlock - 1) / (kUnit * kBlock);
   const long long wgs = static_cast<long long>(n_seqs / group) * p.tiles * c.kv_heads;
-  const long long want = kCus * waves_per_simd(c.type, c.dh) / wgs, most = units / kMinUnits;
-  p.splits = static_cast<int>(want < most ? want : most);
-  if (p.splits < 1) p.splits = 1;
+  const long long want = kCus * waves_per_simd(c.type, c.dh) / wgs;
+  p.splits = static_cast<int>(want < units ? want : units);
+  if (units < kSplitUnits || p.splits < 1) p.splits = 1;
   return p;
 }
 
