@@ -415,8 +415,10 @@ enum { PD_INT4 = 2 };
  *            the parents that pd_pages_fork takes.  A place no candidate is
  *            left for has score -inf, parent -1, token pad_id, length 0, done 1.
  *            out_scores, out_len, out_done may be scores, lens, done themselves.
+ *            Scores below float's lowest value are stored as that value.
  *   out_flags device [B]: PD_FLAG_NONFINITE if a live beam had a NaN or +inf logit
- * 1 <= beam <= 64; vocab <= 2^24 (fewer words than beams are allowed).
+ * 1 <= beam <= 64, B * beam <= 2^20, vocab <= 2^24 (fewer words than beams are
+ * allowed).
  */
 pd_status pd_beam_select_bytes(int32_t dtype, int32_t B, int32_t beam, int32_t vocab, size_t* bytes);
 pd_status pd_beam_select(const void* logits, int32_t dtype, int64_t ld, int32_t B, int32_t beam, int32_t vocab,
@@ -469,12 +471,14 @@ pd_status pd_cache_bytes(const pd_cache* cache, size_t* kv_bytes, size_t* scale_
  *            one sequence alone (as pd_pages_fork leaves it).
  *   table    device int32 [n_seqs][table_ld] page ids, lens device int32
  *            [n_seqs].  A length counts up to max_len (host) and the table's
- *            row; keys of a page id outside the pool are left out and nothing
- *            is written there.  A row with no keys comes out zero.
+ *            row (a longer one's new key and value are not written); keys of a
+ *            page id outside the pool are left out and nothing is written
+ *            there.  A row with no keys, or whose scores all overflow to -inf,
+ *            comes out zero.
  *   group    the n_seqs sequences come in groups of this many (the beams of a
  *            sentence) which are evaluated together, a page that several of
  *            them share being read once.  Affects speed only (and rounding).
- * out must not overlap any other buffer of the call.
+ * n_seqs * heads <= 2^22.  out must not overlap any other buffer of the call.
  */
 pd_status pd_cache_attend_bytes(const pd_cache* cache, int32_t heads, int32_t n_seqs, int32_t group, int32_t max_len,
                                 size_t* bytes);
@@ -539,7 +543,9 @@ pd_status pd_pages_compact(const pd_cache* cache, const int32_t* table, int32_t 
  * step a decoder forward of B * beam rows (self-attention over a paged cache
  * whose pages the beams of a sentence share, cross-attention to the sentence's
  * encoder memory), pd_beam_select and pd_pages_fork, captured as a graph.
- *   beam        hypotheses per sentence, 1 .. 64 (1: greedy decoding)
+ *   beam        hypotheses per sentence, 1 .. 64 (1: greedy decoding); the
+ *               context's max_batch * beam at most 2^20, times the heads 2^22,
+ *               times ceil(max_tgt / 16) 2^24
  *   alpha       length normalisation: hypotheses are ranked by
  *               score / length^alpha (finite, >= 0)
  *   cache_dtype storage of the self-attention cache: the model's dtype or PD_INT4

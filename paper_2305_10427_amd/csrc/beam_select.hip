@@ -415,7 +415,8 @@ __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const Select
     const int tok = !there || fin ? a.pad_id : key_word(sm.key[k][r]);
     const int len = there ? sm.len[k] : 0;
     const int done = !there || fin || tok == a.eos_id || (a.max_len != nullptr && len >= a.max_len[b]) ? 1 : 0;
-    a.out_scores[o] = there ? static_cast<float>(cum_of(k, r)) : -INFINITY;
+    // a sum of lowest values stays finite, so that a hypothesis never turns into none
+    a.out_scores[o] = there ? fmaxf(static_cast<float>(cum_of(k, r)), -3.4028235e38f) : -INFINITY;
     a.out_parent[o] = k;
     a.out_token[o] = tok;
     a.out_len[o] = len;

@@ -172,8 +172,8 @@ template <int DH> struct AppendRow {
     const size_t x0 = static_cast<size_t>(seq0 + r) * a.new_ld + static_cast<size_t>(kv) * DH + d;
     if (a.new_bf16) Vec16<bf16_t>::load(static_cast<const bf16_t*>(src), x0, x);
     else load_n<float, 8>(static_cast<const float*>(src), x0, x);
-    pos = keys_of(a.lens, seq0 + r, a.max_len, a.table_ld, a.c.ps) - 1;
-    pos = in ? pos : -1;
+    const int n = keys_of(a.lens, seq0 + r, a.max_len, a.table_ld, a.c.ps);
+    pos = in && a.lens[seq0 + r] == n ? n - 1 : -1;      // a length that was cut has its last position elsewhere
   }
 };
 
@@ -650,10 +650,11 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
       mx = xor32_max(xor16_max(mx));
       const float mn = fmaxf(m, mx);
       const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      const float top = mn == -INFINITY ? 0.f : mn;       // scores that overflowed have no weight
       float p[8], sum = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        p[j] = __builtin_amdgcn_exp2f(sc[j] - mn);         // 0 for a key that does not exist
+        p[j] = __builtin_amdgcn_exp2f(sc[j] - top);        // 0 for a key that does not exist
         sum += p[j];
       }
       // --- weights times V ---

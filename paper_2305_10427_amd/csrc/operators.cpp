@@ -29,6 +29,7 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 }
 
 constexpr long long kMaxRows = 1LL << 22;        // workgroups of the largest launch
+constexpr long long kMaxBeams = 1LL << 20;       // of the selection, whose workgroups are larger
 constexpr long long kMaxPositions = 1LL << 30;   // tokens a table row can name
 
 // The shape of a cache (its buffers aside).
@@ -96,8 +97,8 @@ pd_status check_select(int32_t dtype, int32_t B, int32_t beam, int32_t vocab) {
   if (dtype != PD_F32 && dtype != PD_BF16) return fail(PD_E_ARG, "logits must be PD_F32 or PD_BF16");
   if (B < 1 || beam < 1 || vocab < 1) return fail(PD_E_ARG, "B, beam and vocab must be >= 1");
   if (beam > kMaxBeam) return fail(PD_E_SHAPE, "at most 64 beams");
-  if (vocab > (1 << 24) || static_cast<long long>(B) * beam > kMaxRows)
-    return fail(PD_E_SHAPE, "vocab exceeds 2^24 or B * beam exceeds 2^22");
+  if (vocab > (1 << 24) || static_cast<long long>(B) * beam > kMaxBeams)
+    return fail(PD_E_SHAPE, "vocab exceeds 2^24 or B * beam exceeds 2^20");
   return PD_OK;
 }
 
@@ -210,7 +211,7 @@ pd_status pd_cache_read(const pd_cache* cache, int32_t layer, const int32_t* tab
   if ((st = check_table(cache, table, table_ld, lens, n_seqs)) != PD_OK) return st;
   if (first == nullptr || out_k == nullptr || out_v == nullptr) return fail(PD_E_ARG, "null argument");
   if (count < 1) return fail(PD_E_ARG, "count must be >= 1");
-  if (count > kMaxPositions) return fail(PD_E_SHAPE, "count exceeds 2^30");
+  if (static_cast<long long>(n_seqs) * count > (1LL << 40)) return fail(PD_E_SHAPE, "n_seqs * count exceeds 2^40");
   const ReadArgs a{view(cache), layer, table, table_ld, lens, n_seqs, first, count, out_k, out_v};
   return launched(launch_cache_read(a, static_cast<hipStream_t>(stream)), "cache read");
 }

@@ -874,8 +874,8 @@ pd_status check_beam(const pd_ctx* ctx, int32_t beam, int32_t cache_dtype) {
     return fail(PD_E_ARG, "cache_dtype must be the model's dtype or PD_INT4");
   const long long R = static_cast<long long>(ctx->max_batch) * beam;
   const long long ld = (ctx->max_tgt + kBeamPage - 1) / kBeamPage;
-  if (R * ctx->M->H > (1LL << 22) || R * ld > (1LL << 24))
-    return fail(PD_E_SHAPE, "max_batch * beam is too large: at most 2^22 rows times heads and 2^24 pages");
+  if (R > (1LL << 20) || R * ctx->M->H > (1LL << 22) || R * ld > (1LL << 24))
+    return fail(PD_E_SHAPE, "max_batch * beam is too large: at most 2^20 rows, 2^22 rows times heads and 2^24 pages");
   return PD_OK;
 }
 

@@ -296,14 +296,19 @@ class Context:
         ws, need = self._beam_ws[key]
         B, m_max = len(tgt_m), max(tgt_m, default=0)
         rows = max(B, 1)                     # nothing encoded: the library itself reports it
-        ids = torch.empty((rows, beam, max(m_max, 1)), dtype=torch.int32, device=self.device)
-        ln = torch.empty((rows, beam), dtype=torch.int32, device=self.device)
-        scores = torch.empty((rows, beam), dtype=torch.float32, device=self.device)
-        k, fl = (torch.empty(rows, dtype=torch.int32, device=self.device) for _ in range(2))
-        _check(L.pd_decode_beam(self.handle, int(beam), float(alpha), dt, _host_i32(tgt_m), ids.data_ptr(), ids.shape[2],
-                                ln.data_ptr(), scores.data_ptr(), k.data_ptr(), fl.data_ptr(),
-                                (ws.data_ptr() + 255) // 256 * 256, need, _stream_handle(stream)))
-        return ids, ln, scores, k, fl
+
+        def launch(handle):
+            ws.record_stream(torch.cuda.current_stream(ws.device))
+            ids = torch.empty((rows, beam, max(m_max, 1)), dtype=torch.int32, device=ws.device)
+            ln = torch.empty((rows, beam), dtype=torch.int32, device=ws.device)
+            scores = torch.empty((rows, beam), dtype=torch.float32, device=ws.device)
+            k, fl = (torch.empty(rows, dtype=torch.int32, device=ws.device) for _ in range(2))
+            _check(L.pd_decode_beam(self.handle, int(beam), float(alpha), dt, _host_i32(tgt_m), ids.data_ptr(),
+                                    ids.shape[2], ln.data_ptr(), scores.data_ptr(), k.data_ptr(), fl.data_ptr(),
+                                    (ws.data_ptr() + 255) // 256 * 256, need, handle))
+            return ids, ln, scores, k, fl
+
+        return _on(ws.device, stream, launch)
 
     def decode_traced_static(self, mode, tgt_m: Sequence[int], capacity: int, block: int = 1, max_iters: int = 0,
                              horizon: int = 0, stream=None, stop: str = "block"):
@@ -487,6 +492,8 @@ def beam_select(logits, scores, lens, done, *, eos_id: int = C.EOS_ID, pad_id: i
     the beams of a sentence evenly spaced), scores float32, lens and done int32 [B, beam], max_len int32 [B] or None."""
     import torch
     L = load_library()
+    if not isinstance(scores, torch.Tensor):
+        raise PdError(1, "scores must be a tensor")
     dev = scores.device
     f32, i32 = (torch.float32,), (torch.int32,)
     _tensor("logits", logits, (torch.float32, torch.bfloat16), (None, None, None), dev, contiguous=False)
@@ -554,7 +561,6 @@ class PagedCache:
         self.kv_heads, self.head_dim, self.device = kv_heads, head_dim, dev
         self._c = c
         self._p = ctypes.byref(c)
-        self._need = {}                      # workspace bytes by sizes
 
     def _table(self, table, lens):
         import torch
@@ -567,12 +573,9 @@ class PagedCache:
         return shape
 
     def _bytes(self, fn, *sizes):
-        key = (fn,) + sizes
-        if key not in self._need:
-            n = ctypes.c_size_t()
-            _check(getattr(load_library(), fn)(self._p, *sizes, ctypes.byref(n)))
-            self._need[key] = n.value
-        return self._need[key]
+        n = ctypes.c_size_t()
+        _check(getattr(load_library(), fn)(self._p, *sizes, ctypes.byref(n)))
+        return n.value
 
     def attend(self, q, table, lens, *, layer: int = 0, group: int = 1, max_len: Optional[int] = None, new_k=None,
                new_v=None, out_dtype=None, scale: Optional[float] = None, stream=None):

@@ -205,6 +205,27 @@ def test_steps_launched_directly_equal_captured_ones(monkeypatch):
         np.testing.assert_array_equal(a, b)
 
 
+def test_many_sentences_on_another_stream():
+    f = fixture(C.TINY, 4.0, batch=70, max_src=8, max_tgt=12)
+    srcs, ms = sources(C.TINY, [3 + i % 6 for i in range(70)], 45), [1 + i % 12 for i in range(70)]
+    want = run(f, srcs, ms, beam=4)
+    check(f, srcs[60:64], ms[60:64], tuple(x[60:64] for x in want), 4, 1.0)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        encode(f.ctx, srcs)
+    out = f.ctx.decode_beam(ms, beam=4, stream=s)
+    s.synchronize()
+    for a, b in zip(out, want):
+        np.testing.assert_array_equal(a.cpu().numpy(), b)
+
+
+def test_the_widest_beam():
+    f = fixture(C.TINY, 4.0)
+    srcs, ms = sources(C.TINY, [16, 3], 55), [20, 6]
+    check(f, srcs, ms, run(f, srcs, ms, beam=64, alpha=0.6), 64, 0.6)
+
+
 def test_a_vocabulary_smaller_than_the_beam_and_logits_that_are_not_finite():
     cfg = dataclasses.replace(C.TINY, name="few_words", vocab=7)
     f = fixture(cfg, 0.0, batch=2)

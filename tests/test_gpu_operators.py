@@ -10,6 +10,7 @@ output by that relative to sum_j p_j a_j, plus 2^-17 (weights enter the product
 in two bfloat16 parts, 2^-18), plus (n + 64) u (its own sum).  Storing rounds by
 half a step, finfo(t).eps / 2 of the value.
 """
+import ctypes
 import math
 
 import numpy as np
@@ -270,6 +271,56 @@ def test_append_writes_one_slot_and_attends_to_it(cache, dh, ps, new):
         for n, t in (("k", k), ("v", v)):
             ref = pool.take(n, 1, table[s], m)[-1] if m and s != 8 else np.zeros((kv, dh))
             np.testing.assert_array_equal(host(t)[s, 0], ref.astype(np.float32) if cache == "int4" else ref)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16", "int4"])
+def test_append_behind_the_bounds_writes_nothing(cache):
+    """Lengths beyond max_len and beyond the table's row, none, and a page that does not exist."""
+    g = np.random.default_rng(43)
+    ps, kv, dh = 16, 2, 32
+    pool = Pool(g, cache, 1, 12, ps, kv, dh)
+    table = np.arange(12).reshape(6, 2).copy()
+    table[4, 1] = 99
+    lens = [33, 30, 0, -4, 20, 2 ** 31 - 1]
+    before = {n: t.clone() for n, t in pool.tensors().items()}
+    q, new = gpu(g.normal(size=(6, 2, dh)), torch.float32), gpu(g.normal(size=(6, kv, dh)), torch.float32)
+    out = pool.cache.attend(q, i32(table), i32(lens), max_len=29, new_k=new, new_v=new)
+    for n, t in pool.tensors().items():
+        assert torch.equal(t, before[n]), n
+    check(pool, out, q, table, lens, cut=29)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16"])
+def test_scores_that_overflow(cache):
+    """Scores of -inf have no weight, also where a whole block has no other; a row of nothing else is zero."""
+    g = np.random.default_rng(44)
+    ps, kv, dh, ld = 32, 1, 16, 40
+    pool = Pool(g, cache, 1, 3 * ld, ps, kv, dh)
+    low = torch.zeros(3 * ld, dtype=torch.bool)
+    low[torch.from_numpy(g.permutation(2 * ld)[:ld])] = True          # random pages of the first two sequences
+    low[2 * ld:] = True
+    pool.cache.k[0, low.cuda()] = -2.0 ** 100
+    table = np.arange(3 * ld).reshape(3, ld)
+    lens = [ld * ps, 5 * ps + 3, 2 * ps]
+    if low[ld:ld + 6].all() or low[:ld].all():
+        low[ld] = low[0] = False
+    q = gpu(2.0 ** 30 * np.ones((3, 1, dh)), torch.float32)             # 16 * 2^130 / 4: beyond float's range
+    # the other keys' scores are made small again
+    pool.cache.k[0, (~low).cuda()] = (pool.cache.k[0, (~low).cuda()].float() * 2.0 ** -30).to(pool.cache.k.dtype)
+    out = host(pool.cache.attend(q, i32(table), i32(lens)))
+    k, v = host(pool.cache.k)[0, :, 0], host(pool.cache.v)[0, :, 0].swapaxes(-1, -2)
+    for s in range(2):
+        keep = np.repeat(~low.numpy()[table[s]], ps)[:lens[s]]
+        ks, vs = k[table[s]].reshape(-1, dh)[:lens[s]][keep], v[table[s]].reshape(-1, dh)[:lens[s]][keep]
+        sc = ks @ (2.0 ** 30 * np.ones(dh)) / 4
+        p = np.exp(sc - sc.max())
+        want, n = p @ vs / p.sum(), keep.sum()
+        # a score's error: (dh + 8) roundings of a sum of 16 products, relative to the sum of their magnitudes
+        ds = (dh + 8) * 2 * U * (np.abs(ks) @ (2.0 ** 30 * np.ones(dh)) / 4).max()
+        rel = 2 * ds + 2.0 ** -21 + (lens[s] + 64) * U
+        tol = (2 * rel + 2.0 ** -17 + (lens[s] + 64) * U) * (p @ np.abs(vs) / p.sum()) + np.abs(want) * U
+        assert n > 0 and (np.abs(out[s, 0] - want) <= tol).all()
+    assert not out[2].any()
 
 
 def test_append_of_values_that_are_not_finite_and_of_constants():
@@ -539,6 +590,31 @@ def test_selection_of_logits_that_are_not_finite():
         assert r.flags.tolist() == [8, 8, 0, 0, 8, 0]
 
 
+def test_selection_of_lowest_values():
+    """Words masked by the type's lowest value: their hypotheses stay, with finite scores, behind the others."""
+    low = torch.finfo(torch.float32).min
+    x = torch.full((1, 3, 50), low, device="cuda")
+    x[0, 0, 7] = 1.0
+    scores = torch.tensor([[0.0, -math.inf, -math.inf]], device="cuda")
+    lens, done = i32([[0, 0, 0]]), i32([[0, 0, 0]])
+    for alpha in (0.0, 1.0):
+        r = pdec.beam_select(x, scores, lens, done, eos_id=2, pad_id=0, alpha=alpha)
+        assert r.tokens.tolist() == [[7, 0, 1]] and r.parents.tolist() == [[0, 0, 0]] and r.src.tolist() == [[0, 0, 0]]
+        assert r.scores[0, 0] == 0 and (r.scores[0, 1:] == low).all()
+        y = torch.where(torch.arange(50, device="cuda") == 9, 1.0, low).expand(1, 3, 50).contiguous()
+        y[0, 1:] = low
+        y[0, 1:, 30] = 0.0
+        y[0, 1:, 31:] = -math.inf
+        r2 = pdec.beam_select(y, r.scores, r.lens, r.done, eos_id=2, pad_id=0, alpha=alpha)
+        assert r2.tokens[0, 0] == 9 and r2.parents[0, 0] == 0 and (r2.scores[0, 1:] == low).all() and not r2.done.any()
+        assert (r2.parents >= 0).all()
+    # a sum of two of them is below float's range
+    y = torch.tensor([[[0.0, low], [0.0, low]]], device="cuda")
+    r = pdec.beam_select(y, torch.tensor([[low, -math.inf]], device="cuda"), i32([[1, 0]]), i32([[0, 0]]), eos_id=9, pad_id=0,
+                         alpha=0.0)
+    assert r.tokens.tolist() == [[0, 1]] and (r.scores == low).all() and r.parents.tolist() == [[0, 0]]
+
+
 def test_selection_strides_alignment_and_places():
     g = np.random.default_rng(23)
     B, K, V = 3, 5, 1003
@@ -676,6 +752,52 @@ def test_calls_on_another_stream():
         for got in a:
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
         assert torch.equal(f.table, t) and torch.equal(f.lens, n)
+
+
+def test_wrappers_refuse():
+    c = pdec.PagedCache("bf16", 2, 8, 16, 2, 32)
+    t, n = torch.zeros(4, 3, dtype=torch.int32, device="cuda"), torch.ones(4, dtype=torch.int32, device="cuda")
+    q = torch.zeros(4, 4, 32, device="cuda")
+    nk = torch.zeros(4, 2, 32, device="cuda")
+    bad = [lambda: c.attend(q.half(), t, n), lambda: c.attend(q[:3], t, n), lambda: c.attend(q[..., :16], t, n),
+           lambda: c.attend(q.transpose(0, 1), t, n), lambda: c.attend(q[0], t, n), lambda: c.attend(q.cpu(), t, n),
+           lambda: c.attend(q, t.long(), n), lambda: c.attend(q, t, n.cpu()), lambda: c.attend(q, t[0], n),
+           lambda: c.attend(q, t[:, :2], n), lambda: c.attend(q, t, n, group=3), lambda: c.attend(q, t, n, layer=2),
+           lambda: c.attend(q, t, n, new_k=nk), lambda: c.attend(q, t, n, new_k=nk, new_v=nk.bfloat16()),
+           lambda: c.attend(q, t, n, new_k=nk[:, :1], new_v=nk[:, :1]), lambda: c.attend(q, t, n, max_len=0),
+           lambda: c.attend(q, t, n, out_dtype=torch.float16), lambda: c.attend(q, t, n, scale=float("nan")),
+           lambda: c.read(t, n, n.long()), lambda: c.read(t, n, n, count=0), lambda: c.read(t, n, n, layer=-1),
+           lambda: c.fork(t, n, n.float()), lambda: c.fork(t, n, n[:0]), lambda: c.fork(t, n[:3], n),
+           lambda: c.fork(t, n, t), lambda: c.compact(t.T, n), lambda: c.compact(t, n[:2]),
+           lambda: pdec.PagedCache("bf16", 2, 8, 16, 2, 32, k_scale=nk), lambda: pdec.PagedCache("int4", 0, 8, 16, 2, 32)]
+    x, s, i = torch.zeros(2, 3, 9, device="cuda"), torch.zeros(2, 3, device="cuda"), torch.zeros(2, 3, dtype=torch.int32, device="cuda")
+    bad += [lambda: pdec.beam_select(x.half(), s, i, i), lambda: pdec.beam_select(x[..., ::2], s, i, i),
+            lambda: pdec.beam_select(x[:, :2], s, i, i), lambda: pdec.beam_select(x, s.double(), i, i),
+            lambda: pdec.beam_select(x, s, i[:1], i), lambda: pdec.beam_select(x, s, i, i.cpu()),
+            lambda: pdec.beam_select(x, s, i, i, alpha=-1.0), lambda: pdec.beam_select(x, s, i, i, max_len=i),
+            lambda: pdec.beam_select(x[:, :0], s[:, :0], i[:, :0], i[:, :0]), lambda: pdec.beam_select(x, None, i, i)]
+    for k, f in enumerate(bad):
+        with pytest.raises(pdec.PdError):
+            f()
+            pytest.fail(f"call {k} was not refused")
+
+
+def test_compaction_in_place():
+    g = np.random.default_rng(41)
+    table, lens = fork_state(g, 20, 5, 16, 150, 0.4)
+    pool = Pool(g, "bf16", 1, 150, 16, 1, 16)
+    t, n = i32(table), i32(lens)
+    want = R.compact(table, lens, 150, 16)
+    L = pdec.load_library()
+    need = ctypes.c_size_t()
+    assert L.pd_pages_bytes(pool.cache._p, 20, ctypes.byref(need)) == 0
+    ws = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+    remap, st = torch.empty(150, dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+    assert L.pd_pages_compact(pool.cache._p, t.data_ptr(), 5, n.data_ptr(), 20, t.data_ptr(), remap.data_ptr(),
+                              st.data_ptr(), ws.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream) == 0
+    np.testing.assert_array_equal(host(t), want[0])
+    np.testing.assert_array_equal(host(remap), want[1])
+    assert st.tolist() == want[2]
 
 
 def test_results_do_not_change_from_call_to_call():
