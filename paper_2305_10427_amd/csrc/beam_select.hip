@@ -290,14 +290,16 @@ __device__ __forceinline__ u64 double_key(double d) {
   return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
 
-struct MergeLds {
-  u64 key[kMaxBeam][kMaxBeam];      // a beam's best numbers, best first
-  double lse[kMaxBeam], div[kMaxBeam];
-  float score[kMaxBeam];
-  int n[kMaxBeam];                  // a beam's candidates
-  int len[kMaxBeam];                // their length
-  int fin[kMaxBeam];
-  int at_beam[kMaxBeam], at_rank[kMaxBeam];
+// Up to KM beams.
+template <int KM> struct MergeLds {
+  u64 key[KM][KM];                  // a beam's best numbers, best first
+  u64 by[KM][KM];                   // double_key of what they are ranked by
+  double lse[KM];
+  float score[KM];
+  int n[KM];                  // a beam's candidates
+  int len[KM];                // their length
+  int fin[KM];
+  int at_beam[KM], at_rank[KM];
   int bad;
 };
 
@@ -307,14 +309,15 @@ struct MergeLds {
 // each with its best candidate that is left, the largest key and of those the
 // lowest lane first.
 constexpr int kBatch = 6;
+constexpr int kFewBeams = 8;
 
-template <int MW>
-__device__ __forceinline__ void merge_sentence(const SelectArgs& a, const SelectWs& w, int parts, int b, MergeLds& sm,
-                                               u64* buf, int lane, int wave) {
+template <int KM>
+__device__ __forceinline__ void merge_sentence(const SelectArgs& a, const SelectWs& w, int parts, int b, MergeLds<KM>& sm,
+                                               u64* buf, int lane, int wave, int waves) {
   const int K = a.beam;
   if (threadIdx.x == 0) sm.bad = 0;
   __syncthreads();
-  for (int k = wave; k < K; k += MW) {
+  for (int k = wave; k < K; k += waves) {
     const int row = b * K + k;
     const float score = a.scores[row];
     const bool fin = a.done[row] != 0;
@@ -341,6 +344,7 @@ __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const Select
       n = 0;
     } else if (fin) {
       n = 1;
+      if (lane == 0) sm.by[k][0] = double_key(static_cast<double>(score) / div);
     } else {
       if (lane >= parts) mine = PartStat{0.0, -INFINITY, 0};
       for (int p = lane + kWave; p < parts; p += kWave) {
@@ -370,12 +374,15 @@ __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const Select
       }
       best.sort(lane);
       n = best.n;
-      for (int i = lane; i < n; i += kWave) sm.key[k][i] = best.buf[i];
+      for (int i = lane; i < n; i += kWave) {
+        const u64 x = best.buf[i];
+        sm.key[k][i] = x;
+        sm.by[k][i] = double_key((static_cast<double>(score) + (static_cast<double>(key_logit(x)) - lse)) / div);
+      }
     }
     if (lane == 0) {
       sm.n[k] = n;
       sm.lse[k] = lse;
-      sm.div[k] = div;
       sm.score[k] = score;
       sm.len[k] = len;
       sm.fin[k] = fin ? 1 : 0;
@@ -389,7 +396,7 @@ __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const Select
   if (wave == 0) {
     const int k = lane < K ? lane : 0;
     int r = 0;
-    u64 head = lane < K && sm.n[k] > 0 ? double_key(cum_of(k, 0) / sm.div[k]) : 0;
+    u64 head = lane < K && sm.n[k] > 0 ? sm.by[k][0] : 0;
     for (int j = 0; j < K; ++j) {
       const uint32_t hi = static_cast<uint32_t>(head >> 32), hi_max = wave_max_u32(hi);
       u64 vote = __ballot(hi == hi_max);
@@ -402,7 +409,7 @@ __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const Select
         sm.at_beam[j] = head == 0 ? -1 : lane;
         sm.at_rank[j] = r;
         ++r;
-        head = head != 0 && r < sm.n[k] ? double_key(cum_of(k, r) / sm.div[k]) : 0;
+        head = head != 0 && r < sm.n[k] ? sm.by[k][r] : 0;
       }
     }
   }
@@ -426,26 +433,26 @@ __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const Select
   if (t == 0) a.out_flags[b] = sm.bad ? 8 : 0;
 }
 
-template <int MW>
+template <int KM, int MW>
 __global__ __launch_bounds__(MW * kWave) void k_select_merge(SelectArgs a, SelectWs w, int parts) {
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   __shared__ u64 s_buf[MW][kBufKeys];
-  __shared__ MergeLds sm;
-  merge_sentence<MW>(a, w, parts, blockIdx.x, sm, s_buf[wave], lane, wave);
+  __shared__ MergeLds<KM> sm;
+  merge_sentence<KM>(a, w, parts, blockIdx.x, sm, s_buf[wave], lane, wave, MW);
 }
 
-// Both stages of a sentence whose parts are at most as many as a workgroup's waves.
+// Both stages of a sentence of at most kSmallWaves parts, a wave each.
 constexpr int kSmallWaves = 16;
 
 template <typename T>
 __global__ __launch_bounds__(kSmallWaves * kWave) void k_select_small(SelectArgs a, SelectWs w, int parts, int steps) {
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   __shared__ u64 s_buf[kSmallWaves][kBufKeys];
-  __shared__ MergeLds sm;
-  if (wave < a.beam * parts) row_part<T>(a, w, parts, steps, blockIdx.x * a.beam * parts + wave, s_buf[wave], lane);
+  __shared__ MergeLds<kSmallWaves> sm;
+  row_part<T>(a, w, parts, steps, blockIdx.x * a.beam * parts + wave, s_buf[wave], lane);
   __threadfence_block();
   __syncthreads();
-  merge_sentence<kSmallWaves>(a, w, parts, blockIdx.x, sm, s_buf[wave], lane, wave);
+  merge_sentence<kSmallWaves>(a, w, parts, blockIdx.x, sm, s_buf[wave], lane, wave, a.beam * parts);
 }
 
 // Parts of a row and the steps of a part: kWantWaves waves in all where the
@@ -486,7 +493,7 @@ hipError_t launch_beam_select(const SelectArgs& a, hipStream_t s) {
   w.stat = reinterpret_cast<PartStat*>(a.ws);
   w.keys = reinterpret_cast<u64*>(w.stat + units);
   if (a.beam * sp.parts <= kSmallWaves) {
-    const dim3 grid(a.B), block(kSmallWaves * kWave);
+    const dim3 grid(a.B), block(a.beam * sp.parts * kWave);
     if (a.dtype == DT_BF16) hipLaunchKernelGGL(k_select_small<bf16_t>, grid, block, 0, s, a, w, sp.parts, sp.steps);
     else hipLaunchKernelGGL(k_select_small<float>, grid, block, 0, s, a, w, sp.parts, sp.steps);
     return hipGetLastError();
@@ -496,9 +503,8 @@ hipError_t launch_beam_select(const SelectArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL(k_select_rows<float>, grid, block, 0, s, a, w, sp.parts, sp.steps);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.beam <= 4) hipLaunchKernelGGL(k_select_merge<4>, dim3(a.B), dim3(4 * kWave), 0, s, a, w, sp.parts);
-  else if (a.beam <= 8) hipLaunchKernelGGL(k_select_merge<8>, dim3(a.B), dim3(8 * kWave), 0, s, a, w, sp.parts);
-  else hipLaunchKernelGGL(k_select_merge<16>, dim3(a.B), dim3(16 * kWave), 0, s, a, w, sp.parts);
+  if (a.beam <= kFewBeams) hipLaunchKernelGGL((k_select_merge<kFewBeams, kFewBeams>), dim3(a.B), dim3(kFewBeams * kWave), 0, s, a, w, sp.parts);
+  else hipLaunchKernelGGL((k_select_merge<kMaxBeam, 16>), dim3(a.B), dim3(16 * kWave), 0, s, a, w, sp.parts);
   return hipGetLastError();
 }
 
