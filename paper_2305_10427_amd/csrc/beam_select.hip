@@ -276,6 +276,10 @@ __device__ __forceinline__ void row_part(const SelectArgs& a, const SelectWs& w,
   if (lane == 0) w.stat[out] = PartStat{s, m, any != 0 ? 1 : 0};
 }
 
+// The rows, in one pass over the logits: bound by memory and by the launch's start
+// and end (a wave sorts its list).  64 x 5 rows of 58,101 float32 words, four fifths
+// of them live (59.5 MB): 17.7 us, 3.4 TB/s; 128 rows of 250,027 bfloat16 words (58
+// MB): 20.7 us, 2.8 TB/s; a copy of 1 GB reaches 5.2.
 template <typename T>
 __global__ __launch_bounds__(kRowWaves * kWave) void k_select_rows(SelectArgs a, SelectWs w, int parts, int steps) {
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -307,7 +311,11 @@ template <int KM> struct MergeLds {
 // merges the parts (it requests the statistics and the first kBatch x 64
 // numbers before it uses any); then the first wave merges the beams, a lane
 // each with its best candidate that is left, the largest key and of those the
-// lowest lane first.
+// lowest lane first, from keys that the waves have made for all candidates (of 16
+// beams: 14.1 us a call, 16.3 with the keys made as they come up).  A chain of
+// latencies: 6 .. 7 us.  Up to kFewBeams beams take a workgroup of as many waves and
+// lists of that length: 64 x 5 rows of 58,101 words 23.2 us a call against 23.9 in
+// workgroups for 64 beams, one sentence of them 10.8 against 11.3.
 constexpr int kBatch = 6;
 constexpr int kFewBeams = 8;
 
@@ -441,7 +449,11 @@ __global__ __launch_bounds__(MW * kWave) void k_select_merge(SelectArgs a, Selec
   merge_sentence<KM>(a, w, parts, blockIdx.x, sm, s_buf[wave], lane, wave, MW);
 }
 
-// Both stages of a sentence of at most kSmallWaves parts, a wave each.
+// Both stages of a sentence of at most kSmallWaves parts of one step, a wave each:
+// one launch.  Against two (us a call): 4 rows of 1,000 words 8.3 / 9.1, 64 x 4 rows
+// 8.9 / 9.9, 1,024 x 4 rows 12.3 / 22.1, 64 x 5 rows of 2,999 words 11.6 / 11.3; with
+// more than a step a wave the two are faster: 1,024 x 5 rows of 10,007 words 66.8 /
+// 56.2.
 constexpr int kSmallWaves = 16;
 
 template <typename T>
@@ -456,7 +468,8 @@ __global__ __launch_bounds__(kSmallWaves * kWave) void k_select_small(SelectArgs
 }
 
 // Parts of a row and the steps of a part: kWantWaves waves in all where the
-// rows are long enough, each of at least one step (4 KB).
+// rows are long enough, each of at least one step (4 KB).  Half as many are slower
+// for 320 rows of 58,101 words, twice as many no faster.
 constexpr int kWantWaves = 4096;
 struct Split {
   int parts, steps;
@@ -492,7 +505,7 @@ hipError_t launch_beam_select(const SelectArgs& a, hipStream_t s) {
   SelectWs w;
   w.stat = reinterpret_cast<PartStat*>(a.ws);
   w.keys = reinterpret_cast<u64*>(w.stat + units);
-  if (a.beam * sp.parts <= kSmallWaves) {
+  if (a.beam * sp.parts <= kSmallWaves && sp.steps == 1) {
     const dim3 grid(a.B), block(a.beam * sp.parts * kWave);
     if (a.dtype == DT_BF16) hipLaunchKernelGGL(k_select_small<bf16_t>, grid, block, 0, s, a, w, sp.parts, sp.steps);
     else hipLaunchKernelGGL(k_select_small<float>, grid, block, 0, s, a, w, sp.parts, sp.steps);

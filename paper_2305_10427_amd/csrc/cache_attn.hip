@@ -74,8 +74,8 @@ __device__ __forceinline__ uint32_t group_code(float x, float step, float least)
 // --- the tile ------------------------------------------------------------------
 //
 // A workgroup takes up to 16 query rows that read the same key/value head: the
-// beams of a group (RB of them) times the G query heads of the key head, and a
-// range of key blocks of 32 positions.  For each block it finds the distinct
+// beams of a group (up to 16 / G) times the G query heads of the key head, and a
+// part of the key blocks of 32 positions.  For each block it finds the distinct
 // (pages, valid keys) among its beams: beams that share a prefix share one
 // item, so a page is read once however many of them refer to it.  Waves take
 // items in turn; an item's keys are scored against all 16 rows on the matrix
@@ -376,13 +376,23 @@ struct Plan {
   int rows_per_tile, tiles, splits;
 };
 
-// Waves a SIMD is to hold (workgroups a CU), by registers and LDS.
+// Waves a SIMD is to hold (workgroups a CU): what the registers of an instance and
+// its LDS allow without spilling.
 constexpr int waves_per_simd(int ct, int dh) {
   if (ct == CT_F32) return dh >= 128 ? 1 : dh == 64 ? 2 : dh == 32 ? 3 : 4;
   if (ct == CT_BF16) return dh >= 128 ? 1 : dh == 64 ? 3 : 4;
   return dh >= 128 ? 2 : dh == 64 ? 3 : 4;
 }
 
+// Long caches are bound by memory in float32 and bfloat16 (16 rows of 8,191 ..
+// 16,381 keys, 16 heads of 64, bfloat16, 805 MB: 151 us, 5.3 TB/s; reading alone
+// reaches 5.9) and by the vector instructions that unpack in 4 bits (2 x 4 rows of
+// 20,011 .. 32,749 keys, 4 heads of 128 for 16, 44 MB: 27.3 us; 64 x 4 rows of 4,000
+// keys of 64, 312 MB: 112 us, 2.8 TB/s).  Short ones are a chain of latencies -
+// lengths, table, keys, products, the waves' join - of 6 us for one sentence and,
+// with 512 workgroups (64 x 5 rows of 15 .. 138 keys, 8 heads, bfloat16, 29 MB),
+// 15.4 us, of which the append is 1.7: its stores have to land before its keys are
+// read.
 template <int CT, int DH>
 __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(AttendArgs a, Plan pl) {
   constexpr int NU = DH >= 32 ? DH / 32 : 1;          // steps of 32 dimensions (bf16 products), groups of a cache in 4 bits
@@ -806,8 +816,9 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
   }
 }
 
-// The parts of a row's key ranges: a workgroup per row, DH / 4 lanes for each
-// kJoinThreads / (DH / 4)-th of the ranges, then those sums in order.
+// The parts of a row's keys: a workgroup per row, DH / 4 lanes for each
+// kJoinThreads / (DH / 4)-th of the parts, then those sums in order.  4 .. 5 us: a
+// launch and two rounds of loads.
 constexpr int kJoinThreads = 256;
 
 template <int DH>
