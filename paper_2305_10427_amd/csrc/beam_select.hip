@@ -158,6 +158,9 @@ __device__ __forceinline__ float exp_neg(float d) {
   return __builtin_amdgcn_exp2f(fmaf(d, hi, d * lo));
 }
 
+// A step's exponentials are summed in float, in kSums sums: at most 9 roundings.
+constexpr int kSums = 4;
+
 // One step of a lane: NV vectors of E logits of the row, whose words start at
 // word0 and lie `apart` apart (those that do not exist: -inf).  A NaN or +inf makes the sum NaN,
 // which is seen afterwards: then those logits are left out and the step is
@@ -170,9 +173,10 @@ __device__ __forceinline__ void take_step(const T* row, float* x, int word0, int
 #pragma unroll
     for (int i = 1; i < NV * E; ++i) top = fmaxf(top, x[i]);
     m = fmaxf(ls.max, top);
-    sum = 0.f;
+    float part[kSums] = {};
 #pragma unroll
-    for (int i = 0; i < NV * E; ++i) sum += exp_neg(x[i] - m);
+    for (int i = 0; i < NV * E; ++i) part[i % kSums] += exp_neg(x[i] - m);
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
   };
   reduce();
   if (!(sum < INFINITY)) {             // something is not finite, or nothing is there yet (-inf - -inf)
