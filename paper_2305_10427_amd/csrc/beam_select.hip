@@ -311,19 +311,23 @@ template <int KM> struct MergeLds {
   int bad;
 };
 
-// The survivors of sentence b, from its rows' part lists.  A wave per beam
-// merges the parts (it requests the statistics and the first kBatch x 64
-// numbers before it uses any); then the first wave merges the beams, a lane
-// each with its best candidate that is left, the largest key and of those the
-// lowest lane first, from keys that the waves have made for all candidates (of 16
-// beams: 14.1 us a call, 16.3 with the keys made as they come up).  A chain of
-// latencies: 6 .. 7 us.  Up to kFewBeams beams take a workgroup of as many waves and
-// lists of that length: 64 x 5 rows of 58,101 words 23.2 us a call against 23.9 in
-// workgroups for 64 beams, one sentence of them 10.8 against 11.3.
-constexpr int kBatch = 6;
-constexpr int kFewBeams = 8;
+// The survivors of sentence b, from its rows' part lists.  A wave per beam merges
+// the parts; then the first wave merges the beams, a lane each with its best
+// candidate that is left, the largest key and of those the lowest lane first, from
+// keys that the waves have made for all candidates (of 16 beams: 14.1 us a call,
+// 16.3 with the keys made as they come up).  A chain of latencies: 6 us.
+//
+// The parts' numbers are read 64 at a time, kBatch of those before any is used: as
+// they lie where they all fit, else (BY_RANK) rank by rank, until a rank has nothing
+// above the bar, nor then have later ones.  5 rows of 250,027 words 13.4 us a call by
+// rank, 15.0 in order; 16 rows 21.9 and 35.6.
+//
+// Up to kFewBeams beams take a workgroup of as many waves and lists of that length:
+// 64 x 5 rows of 58,101 words 23.2 us a call against 23.9 in workgroups for 64
+// beams, one sentence of them 10.8 against 11.3.
+constexpr int kFewBeams = 8, kMergeBatch = 6;
 
-template <int KM>
+template <int KM, int kBatch, bool BY_RANK>
 __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const SelectWs& w, int parts, int b, MergeLds<KM>& sm,
                                                u64* buf, int lane, int wave, int waves) {
   const int K = a.beam;
@@ -335,14 +339,17 @@ __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const Select
     const bool fin = a.done[row] != 0;
     const int len = a.lens[row] + (fin ? 0 : 1);
     const size_t p0 = static_cast<size_t>(row) * parts;
-    const int total = parts * K;
     u64 key[kBatch];
-    auto load = [&](int i0) {
+    const int groups = (parts + kWave - 1) / kWave;
+    auto load = [&](int q0) {         // by rank: reads q0 .. of (rank, 64 parts)
+      int r = BY_RANK ? q0 / groups : 0, g = BY_RANK ? q0 - r * groups : 0;
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
-        const int at = i0 + i * kWave + lane;
-        const u64 x = w.keys[p0 * K + min(at, total - 1)];
-        key[i] = at < total ? x : 0;
+        const int at = BY_RANK ? (g * kWave + lane) * K + r : i * kWave + lane;
+        const bool in = BY_RANK ? g * kWave + lane < parts && r < K : at < parts * K;
+        const u64 x = w.keys[p0 * K + (in ? at : 0)];
+        key[i] = in ? x : 0;
+        if (BY_RANK && ++g == groups) g = 0, ++r;
       }
     };
     load(0);
@@ -373,16 +380,21 @@ __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const Select
       if (__ballot(mine.bad != 0) != 0 && lane == 0) sm.bad = 1;
       WaveBest best;
       best.init(buf, K);
-      for (int i0 = 0; i0 < total; i0 += kBatch * kWave) {
-        if (i0 > 0) load(i0);
+      int idle = 0;                   // reads in turn that held nothing
+      for (int q0 = 0;;) {
         u64 top = key[0];
 #pragma unroll
         for (int i = 1; i < kBatch; ++i) top = key[i] > top ? key[i] : top;
-        if (__ballot(top > best.bar) == 0) continue;
         best.raise(static_cast<uint32_t>(top >> 32));
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i)
-          if (__ballot(key[i] > best.bar) != 0) best.offer(key[i], lane);
+        for (int i = 0; i < kBatch; ++i) {
+          const bool any = __ballot(key[i] > best.bar) != 0;
+          if (any) best.offer(key[i], lane);
+          idle = any ? 0 : idle + 1;
+        }
+        q0 += kBatch;
+        if (!BY_RANK || q0 >= K * groups || idle >= groups) break;
+        load(q0);
       }
       best.sort(lane);
       n = best.n;
@@ -445,12 +457,12 @@ __device__ __forceinline__ void merge_sentence(const SelectArgs& a, const Select
   if (t == 0) a.out_flags[b] = sm.bad ? 8 : 0;
 }
 
-template <int KM, int MW>
+template <int KM, int MW, bool BY_RANK>
 __global__ __launch_bounds__(MW * kWave) void k_select_merge(SelectArgs a, SelectWs w, int parts) {
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   __shared__ u64 s_buf[MW][kBufKeys];
   __shared__ MergeLds<KM> sm;
-  merge_sentence<KM>(a, w, parts, blockIdx.x, sm, s_buf[wave], lane, wave, MW);
+  merge_sentence<KM, kMergeBatch, BY_RANK>(a, w, parts, blockIdx.x, sm, s_buf[wave], lane, wave, MW);
 }
 
 // Both stages of a sentence of at most kSmallWaves parts of one step, a wave each:
@@ -468,7 +480,7 @@ __global__ __launch_bounds__(kSmallWaves * kWave) void k_select_small(SelectArgs
   row_part<T>(a, w, parts, steps, blockIdx.x * a.beam * parts + wave, s_buf[wave], lane);
   __threadfence_block();
   __syncthreads();
-  merge_sentence<kSmallWaves>(a, w, parts, blockIdx.x, sm, s_buf[wave], lane, wave, a.beam * parts);
+  merge_sentence<kSmallWaves, kSmallWaves * kSmallWaves / kWave, false>(a, w, parts, blockIdx.x, sm, s_buf[wave], lane, wave, a.beam * parts);
 }
 
 // Parts of a row and the steps of a part: kWantWaves waves in all where the
@@ -487,6 +499,12 @@ Split split_rows(int dtype, int rows, int vocab) {
   s.steps = (all + parts - 1) / parts;
   s.parts = (all + s.steps - 1) / s.steps;
   return s;
+}
+
+template <int KM, int MW, bool BY_RANK>
+hipError_t launch_merge(const SelectArgs& a, const SelectWs& w, int parts, hipStream_t s) {
+  hipLaunchKernelGGL((k_select_merge<KM, MW, BY_RANK>), dim3(a.B), dim3(MW * kWave), 0, s, a, w, parts);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -520,9 +538,9 @@ hipError_t launch_beam_select(const SelectArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL(k_select_rows<float>, grid, block, 0, s, a, w, sp.parts, sp.steps);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.beam <= kFewBeams) hipLaunchKernelGGL((k_select_merge<kFewBeams, kFewBeams>), dim3(a.B), dim3(kFewBeams * kWave), 0, s, a, w, sp.parts);
-  else hipLaunchKernelGGL((k_select_merge<kMaxBeam, 16>), dim3(a.B), dim3(16 * kWave), 0, s, a, w, sp.parts);
-  return hipGetLastError();
+  const bool by_rank = a.beam * sp.parts > kMergeBatch * kWave;
+  if (a.beam <= kFewBeams) return by_rank ? launch_merge<kFewBeams, kFewBeams, true>(a, w, sp.parts, s) : launch_merge<kFewBeams, kFewBeams, false>(a, w, sp.parts, s);
+  return by_rank ? launch_merge<kMaxBeam, 16, true>(a, w, sp.parts, s) : launch_merge<kMaxBeam, 16, false>(a, w, sp.parts, s);
 }
 
 }  // namespace pdec

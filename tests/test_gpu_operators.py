@@ -592,6 +592,20 @@ def test_selection_orders_of_logits():
                 check_select(r, x.to(dt), scores, lens, done, alpha=0.0)
 
 
+@pytest.mark.parametrize("K,V", [(5, 80003), (11, 40009), (64, 9001)])
+def test_selection_merges_many_parts_in_any_order(K, V):
+    """One sentence, its rows in so many parts that their lists are merged by rank: the best in one part, spread, equal."""
+    g = np.random.default_rng(24)
+    i = np.arange(V)
+    rows = [i * 1e-4, -i * 1e-4, 0 * i, np.where(i >= V - 90, 5.0 + i * 1e-5, -5.0), np.where(i < 90, 5.0, -5.0 - i * 1e-5),
+            (i % 1024 == 7) * 3.0, g.integers(0, 3, V), np.where(i == 77, 1.0, -np.inf), 3 * g.normal(size=V)]
+    for r in rows:
+        x = gpu(np.stack([r] * K)[None], torch.float32)
+        x[0, K // 2] += 0.25
+        scores, lens, done = -0.5 * np.arange(K)[None], np.full((1, K), 3), np.zeros((1, K), int)
+        check_select(run_select(x, scores, lens, done, alpha=0.0), x, scores, lens, done, alpha=0.0)
+
+
 def test_selection_of_logits_that_are_not_finite():
     g = np.random.default_rng(22)
     B, K, V = 6, 4, 2003
