@@ -282,7 +282,7 @@ __device__ __forceinline__ void row_part(const SelectArgs& a, const SelectWs& w,
 
 // The rows, in one pass over the logits: bound by memory and by the launch's start
 // and end (a wave sorts its list).  64 x 5 rows of 58,101 float32 words, four fifths
-// of them live (59.5 MB): 17.7 us, 3.4 TB/s; 128 rows of 250,027 bfloat16 words (58
+// of them live (59.5 MB): 17.5 us, 3.4 TB/s; 128 rows of 250,027 bfloat16 words (58
 // MB): 20.7 us, 2.8 TB/s; a copy of 1 GB reaches 5.2.
 template <typename T>
 __global__ __launch_bounds__(kRowWaves * kWave) void k_select_rows(SelectArgs a, SelectWs w, int parts, int steps) {
@@ -466,10 +466,10 @@ __global__ __launch_bounds__(MW * kWave) void k_select_merge(SelectArgs a, Selec
 }
 
 // Both stages of a sentence of at most kSmallWaves parts of one step, a wave each:
-// one launch.  Against two (us a call): 4 rows of 1,000 words 8.3 / 9.1, 64 x 4 rows
-// 8.9 / 9.9, 1,024 x 4 rows 12.3 / 22.1, 64 x 5 rows of 2,999 words 11.6 / 11.3; with
-// more than a step a wave the two are faster: 1,024 x 5 rows of 10,007 words 66.8 /
-// 56.2.
+// one launch.  Against two (us a call): 4 rows of 1,000 words 7.6 / 8.7, 64 x 4 rows
+// 8.2 / 9.7, 1,024 x 4 rows 11.5 / 16.3, 64 x 5 rows of 2,999 words 11.0 / 11.2; with
+// more than a step a wave the two are faster: 1,024 x 5 rows of 10,007 words 63.9 /
+// 49.0.
 constexpr int kSmallWaves = 16;
 
 template <typename T>

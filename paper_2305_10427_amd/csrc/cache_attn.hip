@@ -385,7 +385,7 @@ constexpr int waves_per_simd(int ct, int dh) {
 }
 
 // Long caches are bound by memory in float32 and bfloat16 (16 rows of 8,191 ..
-// 16,381 keys, 16 heads of 64, bfloat16, 805 MB: 151 us, 5.3 TB/s; reading alone
+// 16,381 keys, 16 heads of 64, bfloat16, 805 MB: 150 us, 5.4 TB/s; reading alone
 // reaches 5.9) and by the vector instructions that unpack in 4 bits (2 x 4 rows of
 // 20,011 .. 32,749 keys, 4 heads of 128 for 16, 44 MB: 27.3 us; 64 x 4 rows of 4,000
 // keys of 64, 312 MB: 112 us, 2.8 TB/s).  Short ones are a chain of latencies -
