@@ -807,6 +807,7 @@ hipError_t take_timing(pd_ctx& C, int slot) {
 
 // --- beam decoding ---
 
+constexpr size_t kBeamGraphs = 64;   // captured steps kept; a call needs two
 constexpr int kBeamPage = 16;     // tokens per page: a copy of a half-filled page moves at most 15 of others' tokens
 
 // Workspace of a beam decode: activations of the rows, the page pool with every
@@ -1304,6 +1305,12 @@ pd_status pd_decode_beam(pd_ctx* ctx, int32_t beam, float alpha, int32_t cache_d
     return fail(PD_E_WORKSPACE, "workspace too small: need " + std::to_string(L.total) + " bytes");
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
+  if (C.beam_graphs.size() + 2 > kBeamGraphs) {   // too many settings so far: start over, once the last call's steps have run
+    const hipError_t e_old = hipEventSynchronize(C.it_ev[0]);
+    if (e_old != hipSuccess) return fail(PD_E_DEVICE, std::string("last decode: ") + hipGetErrorString(e_old));
+    for (auto& bg : C.beam_graphs) hipGraphExecDestroy(bg.exec);
+    C.beam_graphs.clear();
+  }
   if ((st = stage_lengths(ctx, C.stage_tgt, tgt_m, B, C.at<int>(C.L.tgt_m), s)) != PD_OK) return st;
   C.sent_rows = beam;
   auto ints = [&](size_t off) { return reinterpret_cast<int*>(ws + off); };

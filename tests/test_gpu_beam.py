@@ -205,6 +205,18 @@ def test_steps_launched_directly_equal_captured_ones(monkeypatch):
         np.testing.assert_array_equal(a, b)
 
 
+def test_many_settings_of_one_context():
+    """More settings than captured steps are kept for."""
+    f = fixture(C.TINY, 4.0)
+    srcs, ms = sources(C.TINY, [16, 3], 65), [9, 6]
+    alphas = [0.0] + [0.25 + 0.01 * i for i in range(40)]
+    first = run(f, srcs, ms, beam=3, alpha=alphas[0])
+    for a in alphas[1:]:
+        run(f, srcs, ms, beam=3, alpha=a)
+    for a, b in zip(run(f, srcs, ms, beam=3, alpha=alphas[0]), first):
+        np.testing.assert_array_equal(a, b)
+
+
 def test_many_sentences_on_another_stream():
     f = fixture(C.TINY, 4.0, batch=70, max_src=8, max_tgt=12)
     srcs, ms = sources(C.TINY, [3 + i % 6 for i in range(70)], 45), [1 + i % 12 for i in range(70)]

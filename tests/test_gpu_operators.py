@@ -158,6 +158,8 @@ ATTEND = [
     ("bf16", 2, 2, 32, 16, 24, [33] * 24, True, "f32", "f32"),          # more rows than one tile of the matrix cores
     ("int4", 32, 2, 64, 16, 3, [50, 64, 65], True, "f32", "f32"),       # sixteen query heads share a key head
     ("f32", 9, 3, 16, 16, 11, [40] * 22, True, "f32", "f32"),
+    ("bf16", 14, 2, 32, 32, 5, [70] * 5, True, "f32", "f32"),           # 7 and 11 query heads a key head
+    ("int4", 11, 1, 64, 16, 2, [33, 47], True, "bf16", "f32"),
     # a long axis with few rows
     ("bf16", 4, 4, 64, 16, 1, [5003], False, "f32", "f32"),
     ("int4", 8, 2, 128, 64, 2, [9001, 8999], True, "f32", "f32"),
@@ -321,6 +323,30 @@ def test_scores_that_overflow(cache):
         tol = (2 * rel + 2.0 ** -17 + (lens[s] + 64) * U) * (p @ np.abs(vs) / p.sum()) + np.abs(want) * U
         assert n > 0 and (np.abs(out[s, 0] - want) <= tol).all()
     assert not out[2].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_of_a_fused_projection(dtype):
+    """q, new_k and new_v are columns of one buffer, as a fused projection leaves them; rows that are not 16-byte aligned are refused."""
+    g = np.random.default_rng(45)
+    S, H, kv, dh, ps = 5, 4, 2, 32, 16
+    buf = gpu(g.normal(size=(S, (H + 2 * kv) * dh + 8)), TYPES[dtype])
+    heads = lambda x, a, n: x[:, a * dh:(a + n) * dh].unflatten(1, (n, dh))  # noqa: E731
+    q, k, v = heads(buf, 0, H), heads(buf, H, kv), heads(buf, H + kv, kv)
+    lens = [1, 16, 17, 30, 48]
+    table, n = i32(np.arange(15).reshape(5, 3)), i32(lens)
+    state = Pool(np.random.default_rng(46), dtype, 1, 15, ps, kv, dh), Pool(np.random.default_rng(46), dtype, 1, 15, ps, kv, dh)
+    a = state[0].cache.attend(q, table, n, new_k=k, new_v=v)
+    b = state[1].cache.attend(q.contiguous(), table, n, new_k=k.contiguous(), new_v=v.contiguous())
+    assert torch.equal(a, b)
+    for name, t in state[0].tensors().items():
+        assert torch.equal(t, state[1].tensors()[name])
+    for off in (1, 4):                                        # the rows' distance, then their start
+        bad = gpu(g.normal(size=(S, (H + 2 * kv) * dh + off)), TYPES[dtype])
+        with pytest.raises(pdec.PdError):
+            state[0].cache.attend(heads(bad, 0, H), table, n)
+    with pytest.raises(pdec.PdError):
+        state[0].cache.attend(buf[:, 2:2 + H * dh].unflatten(1, (H, dh)), table, n)
 
 
 def test_append_of_values_that_are_not_finite_and_of_constants():
@@ -764,6 +790,37 @@ def test_a_step_in_a_graph_equals_eager_steps():
             assert torch.equal(st_e[n].reshape(-1), res[n].reshape(-1)), (i, n)
         for n in st_g:
             st_g[n].copy_(res[n].reshape(st_g[n].shape))
+
+
+def test_two_graphs_at_once_equal_eager_calls():
+    """Two captured calls with workspaces of their own (parts of the keys, parts of the rows), replayed on two streams."""
+    g = np.random.default_rng(36)
+    pool = Pool(g, "bf16", 1, 400, 16, 2, 64)
+    table, lens = i32(g.permutation(400).reshape(2, 200)), i32([3200, 2900])
+    i = torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    z = torch.zeros(2, 1, device="cuda")
+    args = [(gpu(g.normal(size=(2, 4, 64)), torch.float32), gpu(3 * g.normal(size=(2, 1, 30011)), torch.float32)) for _ in range(2)]
+    run = lambda q, x: (pool.cache.attend(q, table, lens), *pdec.beam_select(x, z, i, i))  # noqa: E731
+    want = [run(*a) for a in args]
+    graphs = []
+    for a in args:
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = run(*a)
+        graphs.append((graph, out, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for graph, out, s in graphs:
+            for t in out:
+                t.zero_()
+        torch.cuda.synchronize()
+        for graph, _, s in graphs:
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        for (_, out, _), w in zip(graphs, want):
+            assert all(torch.equal(a, b) for a, b in zip(out, w))
 
 
 def test_calls_on_another_stream():
