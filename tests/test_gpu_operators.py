@@ -6,9 +6,10 @@ products in float of exact cache values: off by at most
 magnitudes the linear form adds up, at most (64 + code) step + |least| (a code c
 enters the products as 16 + c, and 16 or 23.5 steps are taken off again).  A weight is then off by twice the largest such
 error, plus 2^-21 (exponentials), plus (n + 64) u (the sum of n weights), and the
-output by that relative to sum_j p_j a_j, plus 2^-17 (weights enter the product
-in two bfloat16 parts, 2^-18), plus (n + 64) u (its own sum).  Storing rounds by
-half a step, finfo(t).eps / 2 of the value.
+output by that relative to sum_j p_j a_j, plus 2^-17 where it is stored in
+bfloat16 (weights enter the product in two bfloat16 parts, 2^-18) or 2^-23 in
+float (three, 2^-25), plus (n + 64) u (its own sum).  Storing rounds by half a
+step, finfo(t).eps / 2 of the value.
 """
 import ctypes
 import math
@@ -121,7 +122,8 @@ def bound(pool, layer, q, ref, w, row, n, scale, out_dtype):
     for h in range(H if m else 0):
         ds = (pool.dh + 8) * 2 * U * abs(scale) * (ak[:, h // (H // kv)] @ np.abs(q[h]))
         rel = 2 * ds.max() + 2.0 ** -21 + (m + 64) * U
-        tol[h] = (2 * rel + 2.0 ** -17 + (m + 64) * U) * (w[h] @ av[:, h // (H // kv)])
+        parts = 2.0 ** -17 if out_dtype == torch.bfloat16 else 2.0 ** -23
+        tol[h] = (2 * rel + parts + (m + 64) * U) * (w[h] @ av[:, h // (H // kv)])
     return tol + (np.abs(ref) + tol) * torch.finfo(out_dtype).eps / 2 + 1e-30
 
 
@@ -320,7 +322,7 @@ def test_scores_that_overflow(cache):
         # a score's error: (dh + 8) roundings of a sum of 16 products, relative to the sum of their magnitudes
         ds = (dh + 8) * 2 * U * (np.abs(ks) @ (2.0 ** 30 * np.ones(dh)) / 4).max()
         rel = 2 * ds + 2.0 ** -21 + (lens[s] + 64) * U
-        tol = (2 * rel + 2.0 ** -17 + (lens[s] + 64) * U) * (p @ np.abs(vs) / p.sum()) + np.abs(want) * U
+        tol = (2 * rel + 2.0 ** -23 + (lens[s] + 64) * U) * (p @ np.abs(vs) / p.sum()) + np.abs(want) * U
         assert n > 0 and (np.abs(out[s, 0] - want) <= tol).all()
     assert not out[2].any()
 
