@@ -496,8 +496,9 @@ def beam_select(logits, scores, lens, done, *, eos_id: int = C.EOS_ID, pad_id: i
         raise PdError(1, "scores must be a tensor")
     dev = scores.device
     f32, i32 = (torch.float32,), (torch.int32,)
-    _tensor("logits", logits, (torch.float32, torch.bfloat16), (None, None, None), dev, contiguous=False)
-    B, K, V = logits.shape
+    shape = logits.shape if isinstance(logits, torch.Tensor) and logits.dim() == 3 else (None, None, None)
+    _tensor("logits", logits, (torch.float32, torch.bfloat16), shape, dev, contiguous=False)
+    B, K, V = shape
     ld = logits.stride(1) if K > 1 else logits.stride(0) if B > 1 else V
     if (V > 1 and logits.stride(2) != 1) or (B > 1 and logits.stride(0) != K * ld):
         raise PdError(1, "the rows of logits must be contiguous and evenly spaced")
@@ -512,9 +513,9 @@ def beam_select(logits, scores, lens, done, *, eos_id: int = C.EOS_ID, pad_id: i
 
     def launch(handle):
         out = torch.empty_like(scores)
-        ints = torch.empty((5, B, K), dtype=torch.int32, device=dev)
-        flags = torch.empty((B,), dtype=torch.int32, device=dev)
-        ws = torch.empty((n.value,), dtype=torch.uint8, device=dev)
+        ints = lens.new_empty(5, B, K)
+        flags = lens.new_empty(B)
+        ws = lens.new_empty(-(-n.value // 4))
         at, step = ints.data_ptr(), 4 * B * K
         _check(L.pd_beam_select(logits.data_ptr(), dt, ld, B, K, V, scores.data_ptr(), lens.data_ptr(),
                                 done.data_ptr(), None if max_len is None else max_len.data_ptr(), eos_id, pad_id,
@@ -608,12 +609,12 @@ class PagedCache:
         n = self._bytes("pd_cache_attend_bytes", H, S, group, top)
 
         def launch(handle):
-            out = torch.empty((S, H, dh), dtype=odt, device=dev)
-            ws = torch.empty((n,), dtype=torch.uint8, device=dev).data_ptr() if n else None
+            out = torch.empty((S, H, dh), dtype=odt, device=dev) if odt != q.dtype else q.new_empty(S, H, dh)
+            ws = lens.new_empty(-(-n // 4)) if n else None
             _check(L.pd_cache_attend(self._p, layer, q.data_ptr(), int(q.dtype == torch.bfloat16), _rows("q", q), H, kp,
                                      vp, ndt, nld, table.data_ptr(), ld, lens.data_ptr(), S, group, top,
                                      dh ** -0.5 if scale is None else scale, out.data_ptr(),
-                                     int(odt == torch.bfloat16), H * dh, ws, n, handle))
+                                     int(odt == torch.bfloat16), H * dh, None if ws is None else ws.data_ptr(), n, handle))
             return out
 
         return _on(dev, stream, launch)
@@ -629,7 +630,7 @@ class PagedCache:
         def launch(handle):
             shape = (S, max(count, 1), self.kv_heads, self.head_dim)
             k = torch.empty(shape, dtype=torch.float32, device=dev)
-            v = torch.empty(shape, dtype=torch.float32, device=dev)
+            v = torch.empty_like(k)
             _check(load_library().pd_cache_read(self._p, layer, table.data_ptr(), ld, lens.data_ptr(), S,
                                                 first.data_ptr(), count, k.data_ptr(), v.data_ptr(), handle))
             return k, v
@@ -647,9 +648,9 @@ class PagedCache:
         n = self._bytes("pd_pages_bytes", n_out)
 
         def launch(handle):
-            new = torch.empty((n_out, ld), dtype=torch.int32, device=dev)
-            rest = torch.empty((n_out + self.pages + 2,), dtype=torch.int32, device=dev)
-            ws = torch.empty((n,), dtype=torch.uint8, device=dev)
+            new = lens.new_empty(n_out, ld)
+            rest = lens.new_empty(n_out + self.pages + 2)
+            ws = lens.new_empty(-(-n // 4))
             at = rest.data_ptr()
             _check(load_library().pd_pages_fork(self._p, table.data_ptr(), ld, lens.data_ptr(), S, parents.data_ptr(),
                                                 n_out, int(grow), new.data_ptr(), at, at + 4 * n_out,
@@ -666,9 +667,9 @@ class PagedCache:
         n = self._bytes("pd_pages_bytes", S)
 
         def launch(handle):
-            new = torch.empty((S, ld), dtype=torch.int32, device=dev)
-            rest = torch.empty((self.pages + 2,), dtype=torch.int32, device=dev)
-            ws = torch.empty((n,), dtype=torch.uint8, device=dev)
+            new = lens.new_empty(S, ld)
+            rest = lens.new_empty(self.pages + 2)
+            ws = lens.new_empty(-(-n // 4))
             at = rest.data_ptr()
             _check(load_library().pd_pages_compact(self._p, table.data_ptr(), ld, lens.data_ptr(), S, new.data_ptr(), at,
                                                    at + 4 * self.pages, ws.data_ptr(), n, handle))
