@@ -388,17 +388,18 @@ constexpr int waves_per_simd(int ct, int dh) {
 // 16,381 keys, 16 heads of 64, bfloat16, 805 MB: 150 us, 5.4 TB/s; reading alone
 // reaches 5.9) and by the vector instructions that unpack in 4 bits (2 x 4 rows of
 // 20,011 .. 32,749 keys, 4 heads of 128 for 16, 44 MB, float output: 30.5 us; 64 x 4 rows of 4,000
-// keys of 64, 312 MB, bfloat16 output: 112 us, 2.8 TB/s).  Short ones are a chain of latencies -
+// keys of 64, 312 MB: 124 us, 2.5 TB/s).  Short ones are a chain of latencies -
 // lengths, table, keys, products, the waves' join - of 6 us for one sentence and,
 // with 512 workgroups (64 x 5 rows of 15 .. 138 keys, 8 heads, bfloat16, 29 MB),
 // 15.4 us, of which the append is 1.7: its stores have to land before its keys are
 // read.
 //
-// Weights enter the product with V in PARTS bfloat16 parts: two (2^-17 of a weight)
-// where the output is rounded to bfloat16 (2^-9), three (float's own 2^-24) where it
-// is float.  The third costs the cache in 4 bits 6 .. 10% (27.5 and 112 us become
-// 30.5 and 124); with two, a float output was off by 1.1e-6, by 2e-7 with three.
-template <int CT, int DH, int PARTS>
+// Weights enter the product with V in three bfloat16 parts, float's own 2^-24,
+// whatever the output's type: with two (2^-17) 1.0e-3 to 1.7e-3 of the bfloat16
+// outputs were not the rounded exact sums, two to three times as many as from plain
+// float.  The third costs the cache in 4 bits up to a tenth (64 x 4 rows of 4,000 keys
+// of 64: 112 and 124 us), the others at most 0.5 us a call.
+template <int CT, int DH>
 __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(AttendArgs a, Plan pl) {
   constexpr int NU = DH >= 32 ? DH / 32 : 1;          // steps of 32 dimensions (bf16 products), groups of a cache in 4 bits
   constexpr int NT = DH / 16;                         // tiles of 16 dimensions
@@ -705,18 +706,15 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
         for (int j = 0; j < 8; ++j) r[j] = p[j];
         take_off(r, hi);
         const uint4 lo = pack8(r);
-        uint4 lo2 = lo;
-        if constexpr (PARTS == 3) {
-          take_off(r, lo);
-          lo2 = pack8(r);
-        }
+        take_off(r, lo);
+        const uint4 lo2 = pack8(r);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           uint4 x = *reinterpret_cast<const uint4*>(v_lds + t * 16 * SG::kSegLds);
           if (!whole) x = make_uint4(x.x & mk.x, x.y & mk.y, x.z & mk.z, x.w & mk.w);
           o[t] = mma_bf16(x, hi, floatx4_t{0.f, 0.f, 0.f, 0.f});
           o[t] = mma_bf16(x, lo, o[t]);
-          if constexpr (PARTS == 3) o[t] = mma_bf16(x, lo2, o[t]);
+          o[t] = mma_bf16(x, lo2, o[t]);
         }
       } else {
         const uint4 off = make_uint4(kMinusMid2, kMinusMid2, kMinusMid2, kMinusMid2);
@@ -744,19 +742,16 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
           const uint4 lo = pack8(r);
           floatx4_t base = mma_bf16(off, hi, floatx4_t{0.f, 0.f, 0.f, 0.f});
           base = mma_bf16(off, lo, base);
-          uint4 lo2 = lo;
-          if constexpr (PARTS == 3) {
-            take_off(r, lo);
-            lo2 = pack8(r);
-            base = mma_bf16(off, lo2, base);
-          }
+          take_off(r, lo);
+          const uint4 lo2 = pack8(r);
+          base = mma_bf16(off, lo2, base);
           constexpr int o0 = kByGroup ? 0 : u * NG;
 #pragma unroll
           for (int t = 0; t < NG; ++t) {
             const uint4 w = codes_bf16(*reinterpret_cast<const uint32_t*>(v_lds + (u * NG + t) * 16 * SG::kSegLds), cm, ce);
             o[o0 + t] = mma_bf16(w, hi, base);
             o[o0 + t] = mma_bf16(w, lo, o[o0 + t]);
-            if constexpr (PARTS == 3) o[o0 + t] = mma_bf16(w, lo2, o[o0 + t]);
+            o[o0 + t] = mma_bf16(w, lo2, o[o0 + t]);
           }
           if constexpr (kByGroup) {
             if (own) {
@@ -935,8 +930,7 @@ template <int CT, int DH>
 hipError_t launch_attend_t(const AttendArgs& a, const Plan& p, hipStream_t s) {
   const long long wgs = static_cast<long long>(a.n_seqs / a.group) * p.tiles * a.c.kv_heads * p.splits;
   const dim3 grid(static_cast<unsigned>(wgs)), block(kThreads);
-  if (CT == CT_F32 || a.out_bf16) hipLaunchKernelGGL((k_attend<CT, DH, 2>), grid, block, 0, s, a, p);
-  else hipLaunchKernelGGL((k_attend<CT, DH, CT == CT_F32 ? 2 : 3>), grid, block, 0, s, a, p);
+  hipLaunchKernelGGL((k_attend<CT, DH>), grid, block, 0, s, a, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL(k_join<DH>, dim3(a.n_seqs * a.heads), dim3(kJoinThreads), 0, s, a, p.splits);
