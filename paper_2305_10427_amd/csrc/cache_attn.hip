@@ -120,6 +120,26 @@ __device__ __forceinline__ float xor32_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Sum of the two doubles of which lo and hi hold the words.
+template <typename P> __device__ __forceinline__ double pair_sum(const P& lo, const P& hi) {
+  auto at = [&](int i) { return __longlong_as_double(static_cast<long long>(static_cast<uint64_t>(hi[i]) << 32 | lo[i])); };
+  return at(0) + at(1);
+}
+__device__ __forceinline__ double xor16_sum_d(double v) {
+  const uint64_t u = static_cast<uint64_t>(__double_as_longlong(v));
+  const auto lo = __builtin_amdgcn_permlane16_swap(static_cast<uint32_t>(u), static_cast<uint32_t>(u), false, false);
+  const auto hi = __builtin_amdgcn_permlane16_swap(static_cast<uint32_t>(u >> 32), static_cast<uint32_t>(u >> 32), false, false);
+  return pair_sum(lo, hi);
+}
+__device__ __forceinline__ double xor32_sum_d(double v) {
+  const uint64_t u = static_cast<uint64_t>(__double_as_longlong(v));
+  const auto lo = __builtin_amdgcn_permlane32_swap(static_cast<uint32_t>(u), static_cast<uint32_t>(u), false, false);
+  const auto hi = __builtin_amdgcn_permlane32_swap(static_cast<uint32_t>(u >> 32), static_cast<uint32_t>(u >> 32), false, false);
+  return pair_sum(lo, hi);
+}
+
+// A product of bfloat16 parts starts with the smallest: one rounding at the full
+// magnitude instead of one a part.
 __device__ __forceinline__ floatx4_t mma_bf16(uint4 a, uint4 b, floatx4_t c) { return Mma<bf16_t>::step(a, b, c); }
 __device__ __forceinline__ floatx4_t mma_f32(float a, float b, floatx4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -492,22 +512,22 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
   } else {
     // A score is sum_u step (sum_d (16 + code) q - 16 qs) + least qs with qs the
     // sum of q over group u: the last two terms are a product of the key's words
-    // with (-16 qs, qs), a row of lanes for each bfloat16 part of those.
-    float par[8];
+    // with (-16 qs, qs), a row of lanes for each of four bfloat16 parts of those.
+    // The terms are several times the score, so qs is summed in double.
+    double par[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) par[e] = 0.f;
+    for (int e = 0; e < 8; ++e) par[e] = 0.0;
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
       float* v = qv[u];
-      float sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[e] = row_ok && (DH >= 32 || g < 2) ? s2 * v[e] : 0.f;
-        sum += v[e];
-      }
+      for (int e = 0; e < 8; ++e) v[e] = row_ok && (DH >= 32 || g < 2) ? s2 * v[e] : 0.f;
       if constexpr (CT == CT_INT4) {
-        par[2 * u + 1] = xor32_sum(xor16_sum(sum));
-        par[2 * u] = -16.f * par[2 * u + 1];
+        double sum = 0.0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += static_cast<double>(v[e]);
+        par[2 * u + 1] = xor32_sum_d(xor16_sum_d(sum));
+        par[2 * u] = -16.0 * par[2 * u + 1];
       }
 #pragma unroll
       for (int part = 0; part < 3; ++part) {
@@ -517,10 +537,19 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
     }
     if constexpr (CT == CT_INT4) {
 #pragma unroll
-      for (int part = 0; part < 3; ++part) {
-        const uint4 x = pack8(par);
+      for (int part = 0; part < 4; ++part) {
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = static_cast<float>(par[e]);
+        const uint4 x = pack8(f);
         if (g == part) qpar = x;
-        take_off(par, x);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float lo, hi;
+          unpack_pair(w[e / 2], lo, hi);
+          par[e] -= static_cast<double>(e % 2 ? hi : lo);
+        }
       }
     }
   }
@@ -632,7 +661,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
           for (int u = 0; u < NU; ++u) {
             const uint4 x = *reinterpret_cast<const uint4*>(k_lds + t * 16 * SG::kRowLds + 64 * u);
 #pragma unroll
-            for (int part = 0; part < 3; ++part) d = mma_bf16(x, qf[u][part], d);
+            for (int part = 2; part >= 0; --part) d = mma_bf16(x, qf[u][part], d);
           }
         } else {
           const uint32_t* w4 = reinterpret_cast<const uint32_t*>(lds + (16 * t + n) * SG::kRowLds + SG::kRow);
@@ -643,7 +672,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
             floatx4_t x = {0.f, 0.f, 0.f, 0.f};
             const uint4 w = codes_bf16(*reinterpret_cast<const uint32_t*>(k_lds + t * 16 * SG::kRowLds + 16 * u), cm, ce);
 #pragma unroll
-            for (int part = 0; part < 3; ++part) x = mma_bf16(w, qf[u][part], x);
+            for (int part = 2; part >= 0; --part) x = mma_bf16(w, qf[u][part], x);
             each<4>([&](auto i_) {
               constexpr int i2 = decltype(i_)::value, at = (4 * t + i2) * NU + u;
               d[i2] = fmaf(row_lane<at % 16>(kstep[at / 16]), x[i2], d[i2]);
@@ -712,9 +741,9 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
         for (int t = 0; t < NT; ++t) {
           uint4 x = *reinterpret_cast<const uint4*>(v_lds + t * 16 * SG::kSegLds);
           if (!whole) x = make_uint4(x.x & mk.x, x.y & mk.y, x.z & mk.z, x.w & mk.w);
-          o[t] = mma_bf16(x, hi, floatx4_t{0.f, 0.f, 0.f, 0.f});
+          o[t] = mma_bf16(x, lo2, floatx4_t{0.f, 0.f, 0.f, 0.f});
           o[t] = mma_bf16(x, lo, o[t]);
-          o[t] = mma_bf16(x, lo2, o[t]);
+          o[t] = mma_bf16(x, hi, o[t]);
         }
       } else {
         const uint4 off = make_uint4(kMinusMid2, kMinusMid2, kMinusMid2, kMinusMid2);
@@ -740,11 +769,11 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
           const uint4 hi = pack8(r);
           take_off(r, hi);
           const uint4 lo = pack8(r);
-          floatx4_t base = mma_bf16(off, hi, floatx4_t{0.f, 0.f, 0.f, 0.f});
-          base = mma_bf16(off, lo, base);
           take_off(r, lo);
           const uint4 lo2 = pack8(r);
-          base = mma_bf16(off, lo2, base);
+          floatx4_t base = mma_bf16(off, lo2, floatx4_t{0.f, 0.f, 0.f, 0.f});
+          base = mma_bf16(off, lo, base);
+          base = mma_bf16(off, hi, base);
           constexpr int o0 = kByGroup ? 0 : u * NG;
 #pragma unroll
           for (int t = 0; t < NG; ++t) {
