@@ -474,7 +474,14 @@ pd_status pd_cache_bytes(const pd_cache* cache, size_t* kv_bytes, size_t* scale_
  *            row (a longer one's new key and value are not written); keys of a
  *            page id outside the pool are left out and nothing is written
  *            there.  A row with no keys, or whose scores all overflow to -inf,
- *            comes out zero.
+ *            comes out zero.  Infinite keys and values count as such: a score of
+ *            -inf has no weight, one of inf makes its row NaN, a value of inf
+ *            with a weight is inf.
+ *   range    values are summed with weights of up to 1 before the division by
+ *            the weights' sum: where that sum overflows, out is infinite or NaN.
+ *            In 4 bits a score is the difference of terms of up to
+ *            31 |scale| step sum_d |q|, and a value one of 31 step: where those
+ *            overflow, out is NaN.
  *   group    the n_seqs sequences come in groups of this many (the beams of a
  *            sentence) which are evaluated together, a page that several of
  *            them share being read once.  Affects speed only (and rounding).

@@ -145,7 +145,7 @@ __device__ __forceinline__ floatx4_t mma_f32(float a, float b, floatx4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-// Eight floats as bfloat16 parts: v = hi + lo (+ lo2) to 2^-17 (2^-25) of v.
+// Eight floats rounded to bfloat16, and what they leave of v.
 __device__ __forceinline__ uint4 pack8(const float* v) {
   return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
 }
@@ -156,6 +156,27 @@ __device__ __forceinline__ void take_off(float* v, uint4 p) {   // v -= p
     v[2 * j] -= __uint_as_float(w[j] << 16);
     v[2 * j + 1] -= __uint_as_float(w[j] & 0xffff0000u);
   }
+}
+
+// Eight floats in three bfloat16 parts of 8 bits each, exactly: the first two are
+// the largest bfloat16 below the magnitude of what is left (its bits less one, cut),
+// so every part has the value's sign and none is 0 unless the value is (which must
+// not be -0).  A product with an infinite key or value, or one that overflows, is
+// then the same infinity in every part; parts rounded to nearest differ in sign or
+// are 0, and their sum would be NaN.
+__device__ __forceinline__ uint4 pack8_below(const float* v) {
+  uint32_t u[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) u[j] = __builtin_elementwise_sub_sat(__float_as_uint(v[j]), 1u);
+  auto two = [&](int j) { return __builtin_amdgcn_perm(u[j + 1], u[j], 0x07060302u); };
+  return make_uint4(two(0), two(2), two(4), two(6));
+}
+__device__ __forceinline__ void split8(float* v, uint4& p0, uint4& p1, uint4& p2) {
+  p0 = pack8_below(v);
+  take_off(v, p0);
+  p1 = pack8_below(v);
+  take_off(v, p1);
+  p2 = pack8(v);
 }
 
 // The eight codes of a word as bfloat16 16 + code: a code fills the top of the
@@ -501,6 +522,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
   if (a.new_k != nullptr && my_slot(ap.pos)) ap_id = page_at(a.table, a.table_ld, seq0 + ap.r, ap.pos / ps, c.pages);
 
   const float s2 = a.scale * kLog2e;                  // scores come out in units of log 2
+  const float sq = DH >= 32 ? s2 : 0.5f * s2;         // 16 dimensions fill a step of 32 twice, each time by half
   uint4 qf[CT == CT_F32 ? 1 : NU][3];
   floatx4_t q32[NF];
   uint4 qpar = make_uint4(0u, 0u, 0u, 0u);            // 4 bits: what multiplies a key's (step, least) words
@@ -521,7 +543,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
     for (int u = 0; u < NU; ++u) {
       float* v = qv[u];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = row_ok && (DH >= 32 || g < 2) ? s2 * v[e] : 0.f;
+      for (int e = 0; e < 8; ++e) v[e] = row_ok ? sq * v[e] + 0.f : 0.f;   // no -0
       if constexpr (CT == CT_INT4) {
         double sum = 0.0;
 #pragma unroll
@@ -529,11 +551,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
         par[2 * u + 1] = xor32_sum_d(xor16_sum_d(sum));
         par[2 * u] = -16.0 * par[2 * u + 1];
       }
-#pragma unroll
-      for (int part = 0; part < 3; ++part) {
-        qf[u][part] = pack8(v);
-        take_off(v, qf[u][part]);
-      }
+      split8(v, qf[u][0], qf[u][1], qf[u][2]);
     }
     if constexpr (CT == CT_INT4) {
 #pragma unroll
@@ -729,14 +747,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(CT, DH)) void k_attend(Att
           auto two = [&](int j) { return ((live >> j & 1u) ? 0xffffu : 0u) | ((live >> (j + 1) & 1u) ? 0xffff0000u : 0u); };
           mk = make_uint4(two(0), two(2), two(4), two(6));
         }
-        const uint4 hi = pack8(p);
-        float r[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) r[j] = p[j];
-        take_off(r, hi);
-        const uint4 lo = pack8(r);
-        take_off(r, lo);
-        const uint4 lo2 = pack8(r);
+        uint4 hi, lo, lo2;
+        split8(p, hi, lo, lo2);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           uint4 x = *reinterpret_cast<const uint4*>(v_lds + t * 16 * SG::kSegLds);

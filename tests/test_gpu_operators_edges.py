@@ -72,3 +72,61 @@ def test_scores_in_4_bits_take_a_querys_whole_sum(dh):
     z = deviations(pool, q, pool.cache.attend(q, i32(table), i32(lens), scale=scale), table, lens, scale)
     say("deviations", dh, float(np.sqrt((np.array(z) ** 2).mean())), float(np.abs(z).max()))
     assert E.fits(z)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16"])
+@pytest.mark.parametrize("dh", [16, 32, 64, 128])
+def test_infinite_keys_and_values(cache, dh):
+    """A value of inf with a weight is inf, inf and -inf together NaN; a key whose score is -inf has no weight, whether
+    the key is infinite or the finite product overflows however far; a score of inf makes the row NaN."""
+    g = np.random.default_rng(dh)
+    ps, kv, pages = 16, 2, 40
+    top = float(torch.finfo(torch.bfloat16).max)
+    for q_in in (1.0, -0.3, 2.0 ** 30):
+        pool = Pool(g, cache, 1, pages, ps, kv, dh)
+        if abs(q_in) > 1:                                      # scores of the usual keys stay small
+            pool.cache.k.mul_(1 / q_in)
+        lens = [1, 37, 37, 20, 64, 64, 5, 3]
+        table = np.arange(pages).reshape(8, 5)
+        kc, vc = pool.cache.k[0], pool.cache.v[0]              # [pages][kv][ps][dh], [pages][kv][dh][ps]
+        at = lambda s, j: (table[s, j // ps], j % ps)  # noqa: E731
+        for s, j, d, x in ((0, 0, 3, np.inf), (1, 5, 0, -np.inf), (1, 36, 1, np.inf), (2, 3, 2, np.inf), (2, 20, 2, -np.inf)):
+            p, t = at(s, j)
+            vc[p, :, d, t] = x
+        for s, j, x in ((3, 4, -np.inf), (4, 0, -2.0 ** 120), (4, 1, -top), (4, 40, -2.0 ** 100), (6, 2, np.inf)):
+            p, t = at(s, j)
+            kc[p, :, t] = x * np.sign(q_in)
+        for j in range(64):                                    # no key with a weight: the row is zero
+            p, t = at(5, j)
+            kc[p, :, t] = (-np.inf if j % 3 else -top if abs(q_in) > 1 else -np.inf) * np.sign(q_in)
+        for j in range(3):
+            p, t = at(7, j)
+            kc[p, :, t] = -np.inf * np.sign(q_in)
+        q = gpu(np.full((8, 4, dh), q_in), torch.float32)
+        say("infinite", cache, dh, q_in)
+        for group in (1, 4):
+            out = host(pool.cache.attend(q, i32(table), i32(lens), group=group))
+            z = []
+            for s, n in enumerate(lens):
+                row, slot = [at(s, j)[0] for j in range(n)], [j % ps for j in range(n)]
+                for h in range(4):
+                    k, v = host(kc)[row, h // 2, slot], host(vc)[row, h // 2, :, slot]
+                    sc = dh ** -0.5 * (k @ np.full(dh, float(np.float32(q_in))))
+                    sc[sc < -np.finfo(np.float32).max] = -np.inf
+                    if (sc == np.inf).any():
+                        assert np.isnan(out[s, h]).all()
+                        continue
+                    keep = sc > -np.inf
+                    if not keep.any():
+                        assert (out[s, h] == 0).all()
+                        continue
+                    w = np.exp(sc - sc.max()) / np.exp(sc - sc.max()).sum()
+                    assert (w[~np.isfinite(v).all(-1)] > 1e-20).all()      # an infinite value with no weight is not asked
+                    with np.errstate(invalid="ignore"):
+                        want = w[keep] @ v[keep]
+                    usual = np.isfinite(want)
+                    np.testing.assert_array_equal(out[s, h][~usual], want[~usual])
+                    v = np.where(np.isfinite(v), v, 0.0)
+                    ref, sd, _ = E.attend(cache, np.full(dh, float(np.float32(q_in))), k[keep], v[keep], dh ** -0.5)
+                    z.append(((out[s, h] - ref) / sd)[usual])
+            assert E.fits(z)
