@@ -535,7 +535,8 @@ pd_status pd_pages_fork(const pd_cache* cache, const int32_t* table, int32_t tab
 /*
  * Moves the pages in use (those the n_seqs sequences refer to) to the front of
  * the pool, so that they are pages 0 .. used - 1: the i-th lowest used id of at
- * least `used` goes to the i-th lowest free id below it, in every layer.
+ * least `used` goes to the i-th lowest free id below it, in every layer.  A
+ * length counts from 0 up to the table's row.
  *   out_table  device int32 [n_seqs][table_ld]: the table with the new ids
  *              (may be the table itself)
  *   out_remap  device int32 [pages]: the new id of each old page, -1 if free

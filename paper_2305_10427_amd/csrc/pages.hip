@@ -66,14 +66,18 @@ __device__ __forceinline__ int block_scan(int v, int* s, int& total) {
 
 __device__ __forceinline__ int pages_of(int len, int ps) { return (len + ps - 1) / ps; }
 
+// A length within what the table's row names.
+__device__ __forceinline__ int clamped(const PagesArgs& a, int n) {
+  const long long most = static_cast<long long>(a.table_ld) * a.c.ps;
+  return n < 0 ? 0 : n > most ? static_cast<int>(most) : n;
+}
+
 // The parent of output s (-1: none) and its length, both within their ranges.
 __device__ __forceinline__ int parent_of(const PagesArgs& a, int s, int& len) {
   const int p = a.parents[s];
   len = 0;
   if (p < 0 || p >= a.n_in) return -1;
-  const long long most = static_cast<long long>(a.table_ld) * a.c.ps;
-  const int n = a.lens[p];
-  len = n < 0 ? 0 : n > most ? static_cast<int>(most) : n;
+  len = clamped(a, a.lens[p]);
   return p;
 }
 
@@ -280,13 +284,13 @@ __global__ __launch_bounds__(kPlanThreads) void k_compact_plan(PagesArgs a, Page
       for (int k = 0; k < kBatch; ++k) {
         const long long i = min(i0 + k * kPlanThreads, entries - 1);
         id[k] = a.table[i];
-        n[k] = a.lens[i / ld];
+        n[k] = clamped(a, a.lens[i / ld]);
       }
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         const long long i = i0 + k * kPlanThreads;
         if (i >= entries) continue;
-        const bool there = n[k] > 0 && i % ld < pages_of(n[k], ps) && id[k] >= 0 && id[k] < P;
+        const bool there = i % ld < pages_of(n[k], ps) && id[k] >= 0 && id[k] < P;
         f(i, there ? id[k] : -1);
       }
     }

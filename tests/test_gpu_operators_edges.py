@@ -130,3 +130,23 @@ def test_infinite_keys_and_values(cache, dh):
                     ref, sd, _ = E.attend(cache, np.full(dh, float(np.float32(q_in))), k[keep], v[keep], dh ** -0.5)
                     z.append(((out[s, h] - ref) / sd)[usual])
             assert E.fits(z)
+
+
+@pytest.mark.parametrize("pages", [40, 9000])
+def test_compaction_of_lengths_beyond_the_table(pages):
+    """A length names at most the table's row, however large it is, and none if it is negative."""
+    g = np.random.default_rng(pages)
+    ps, ld = 16, 3
+    lens = [2 ** 31 - 1, 2 ** 31 - ps, -2 ** 31, ld * ps + 1, 2 ** 30, 0, -1, ld * ps, 17]
+    table = g.permutation(pages)[:len(lens) * ld].reshape(len(lens), ld)
+    pool = Pool(g, "bf16", 2, pages, ps, 1, 16)
+    before = {n: t.clone() for n, t in pool.tensors().items()}
+    r = pool.cache.compact(i32(table), i32(lens))
+    new, remap, st, mv = R.compact(table, np.clip(lens, 0, ld * ps), pages, ps)
+    np.testing.assert_array_equal(host(r.table), new)
+    np.testing.assert_array_equal(host(r.remap), remap)
+    assert r.status.tolist() == st and st[1] == 5 * ld + 2
+    for n, t in before.items():
+        for a, b in mv:
+            t[:, b] = t[:, a]
+        assert torch.equal(t, pool.tensors()[n])
