@@ -443,8 +443,9 @@ pd_status pd_beam_select(const void* logits, int32_t dtype, int64_t ld, int32_t 
  *              a token's head vector; a code c stands for least + c * step.
  * A written group has least = its minimum rounded down to bfloat16, step = the
  * smallest bfloat16 with 15 step >= maximum - least, and the nearest codes
- * (ties to even): every value within half a step.  A group with a value that
- * is not finite reads back as NaN.
+ * (ties to even): every value within half a step (to float's rounding), values
+ * below bfloat16's lowest counting as that.  A group with a value that is not
+ * finite reads back as NaN; a code above float's largest value reads as that.
  */
 typedef struct {
   int32_t dtype, layers, pages, page_size, kv_heads, head_dim;

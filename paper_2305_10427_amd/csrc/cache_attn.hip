@@ -16,6 +16,8 @@ namespace pdec {
 
 namespace {
 
+constexpr float kFloatMax = 3.4028234664e38f, kBf16Max = 3.3895313892e38f;
+
 __device__ __forceinline__ int nibble_shift(int e) { return 4 * ((e >> 1) + 4 * (e & 1)); }
 
 // Number of keys of sequence s: within max_len and the table's row.
@@ -45,7 +47,10 @@ __device__ __forceinline__ float cache_value(const CacheView& c, size_t hb, int 
   const uint32_t w = reinterpret_cast<const uint32_t*>(base)[i >> 3];
   const uint32_t par = reinterpret_cast<const uint32_t*>(is_v ? c.vs : c.ks)[(hb * c.ps + t) * c.groups + d / 32];
   const float code = static_cast<float>((w >> nibble_shift(static_cast<int>(i & 7))) & 15u);
-  return code * __uint_as_float(par << 16) + __uint_as_float(par & 0xffff0000u);
+  // the product is exact, and within the sum it cannot overflow; the sixteenth
+  // value of a group can lie above float's largest
+  const float x = fmaf(code, __uint_as_float(par << 16), __uint_as_float(par & 0xffff0000u));
+  return x > kFloatMax ? kFloatMax : x;               // NaN stays
 }
 
 // The largest bfloat16 up to x (x itself if it is not finite).
@@ -55,19 +60,23 @@ __device__ __forceinline__ float bf16_down(float x) {
 }
 
 // Step and least value of a group with the extremes lo, hi: the least value is
-// rounded down and the step up to bfloat16, so that the fifteen steps reach hi.
-// The test of the step is an exact product, on halves so that nothing
-// overflows.  A group with a value that is not finite becomes NaN as a whole.
+// rounded down (to bfloat16's lowest at most) and the step up to bfloat16, so that
+// the fifteen steps reach hi; the test of the step is an exact product.  A range
+// beyond float's, and its step, are taken by half.  A group with a value that is
+// not finite becomes NaN as a whole.
 __device__ __forceinline__ void group_params(float lo, float hi, bool finite, float& step, float& least) {
-  least = bf16_down(lo);
-  const float half = hi * 0.5f - least * 0.5f;
-  step = bf16_down(half * (2.f / 15.f));
-  if (step * 7.5f < half) step = __uint_as_float(__float_as_uint(step) + 0x10000u);
+  least = fmaxf(bf16_down(lo), -kBf16Max);
+  const bool wide = hi - least > kFloatMax;
+  const float range = wide ? hi * 0.5f - least * 0.5f : hi - least;
+  step = bf16_down(range * (1.f / 15.f));
+  if (step * 15.f < range) step = __uint_as_float(__float_as_uint(step) + 0x10000u);
+  if (wide) step *= 2.f;
   if (!finite) step = 0.f, least = NAN;
 }
 __device__ __forceinline__ uint32_t group_code(float x, float step, float least) {
   if (!(step > 0.f)) return 0u;
-  const float c = rintf((x - least) / step);
+  const float d = x - least;
+  const float c = rintf(d > kFloatMax ? (x * 0.5f - least * 0.5f) / (step * 0.5f) : d / step);
   return static_cast<uint32_t>(fminf(fmaxf(c, 0.f), 15.f));
 }
 

@@ -150,3 +150,32 @@ def test_compaction_of_lengths_beyond_the_table(pages):
         for a, b in mv:
             t[:, b] = t[:, a]
         assert torch.equal(t, pool.tensors()[n])
+
+
+@pytest.mark.parametrize("dh", [16, 32, 128])
+def test_append_in_4_bits_over_floats_whole_range(dh):
+    """Every finite value is held within half a step of its group, also where the range or fifteen steps are beyond
+    float's largest value; values below bfloat16's lowest count as that."""
+    top, low = float(torch.finfo(torch.float32).max), -float(torch.finfo(torch.bfloat16).max)
+    tiny = 2.0 ** -149
+    w = min(dh, 32)
+    line = lambda a, b: np.linspace(a, b, w)  # noqa: E731
+    rows = [line(-3e38, 3e38), line(-top, top), line(0, top), line(-top, 0), np.full(w, -top), np.full(w, top), line(low, 1e38),
+            np.where(np.arange(w) % 2, 1.0, top), np.where(np.arange(w) % 3, -1.0, -top), line(0, 9 * tiny), line(-5 * tiny, 0),
+            line(2.0 ** -126, 2.0 ** -120), line(-1e-40, 3e-39), np.array([-3e38, 1e38, 3e38, 0.0] * (w // 4)), line(1e38, 1.1e38)]
+    x = np.stack([np.roll(np.tile(r, (2, dh // w)), i, 1) for i, r in enumerate(rows)]).astype(np.float32)    # [S][kv 2][dh]
+    S = len(rows)
+    pool = Pool(np.random.default_rng(dh), "int4", 1, S, 16, 2, dh)
+    t, n = i32(np.arange(S)[:, None]), i32([1 + i for i in range(S)])
+    pool.cache.attend(torch.zeros(S, 2, dh, device="cuda"), t, n, new_k=gpu(x), new_v=gpu(-x))
+    for name, want, got in zip("kv", (x, -x), pool.cache.read(t, n, n - 1)):
+        want, got = np.maximum(want.astype(np.float64), low).reshape(S, 2, -1, w), host(got)[:, 0].reshape(S, 2, -1, w)
+        # bfloat16 below 2^-126: the multiples of 2^-133 (exponent -126, seven places), coarser than eight places of the value
+        small = 2.0 ** -133
+        least = np.minimum(np.maximum(R.bf16_down(want.min(-1)), low), np.floor(want.min(-1) / small) * small)
+        step = np.maximum(R.bf16_up((want.max(-1) - least) / 15), np.ceil((want.max(-1) - least) / 15 / small) * small)
+        # half a step; a difference, its quotient and the value read are rounded (u of the range each, or to a multiple of tiny)
+        tol = (step / 2 + 2.0 ** -24 * (2 * 15 * step + np.abs(want).max(-1)) + tiny)[..., None]
+        err = np.abs(got - want)
+        say(name, dh, float((err / tol).max()))
+        assert np.isfinite(got).all() and (err <= tol).all(), np.argwhere(~(err <= tol))[:5]
