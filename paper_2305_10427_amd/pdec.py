@@ -289,26 +289,28 @@ class Context:
         L = load_library()
         dt = CACHE_TYPES[self.model.cfg.dtype if cache == "native" else cache]
         key = (int(beam), dt)
-        if key not in self._beam_ws:
-            n = ctypes.c_size_t()
-            _check(L.pd_decode_beam_bytes(self.handle, int(beam), dt, ctypes.byref(n)))
-            self._beam_ws[key] = torch.empty(n.value + 256, dtype=torch.uint8, device=self.device), n.value
-        ws, need = self._beam_ws[key]
+        n = ctypes.c_size_t()
+        _check(L.pd_decode_beam_bytes(self.handle, int(beam), dt, ctypes.byref(n)))
+        need = n.value
+        dev = self.workspace.device
         B, m_max = len(tgt_m), max(tgt_m, default=0)
         rows = max(B, 1)                     # nothing encoded: the library itself reports it
 
         def launch(handle):
-            ws.record_stream(torch.cuda.current_stream(ws.device))
-            ids = torch.empty((rows, beam, max(m_max, 1)), dtype=torch.int32, device=ws.device)
-            ln = torch.empty((rows, beam), dtype=torch.int32, device=ws.device)
-            scores = torch.empty((rows, beam), dtype=torch.float32, device=ws.device)
-            k, fl = (torch.empty(rows, dtype=torch.int32, device=ws.device) for _ in range(2))
+            if key not in self._beam_ws:     # here, so that it is allocated on the stream that uses it
+                self._beam_ws[key] = torch.empty(need + 256, dtype=torch.uint8, device=dev)
+            ws = self._beam_ws[key]
+            ws.record_stream(torch.cuda.current_stream(dev))
+            ids = torch.empty((rows, beam, max(m_max, 1)), dtype=torch.int32, device=dev)
+            ln = torch.empty((rows, beam), dtype=torch.int32, device=dev)
+            scores = torch.empty((rows, beam), dtype=torch.float32, device=dev)
+            k, fl = (torch.empty(rows, dtype=torch.int32, device=dev) for _ in range(2))
             _check(L.pd_decode_beam(self.handle, int(beam), float(alpha), dt, _host_i32(tgt_m), ids.data_ptr(),
                                     ids.shape[2], ln.data_ptr(), scores.data_ptr(), k.data_ptr(), fl.data_ptr(),
                                     (ws.data_ptr() + 255) // 256 * 256, need, handle))
             return ids, ln, scores, k, fl
 
-        return _on(ws.device, stream, launch)
+        return _on(dev, stream, launch)
 
     def decode_traced_static(self, mode, tgt_m: Sequence[int], capacity: int, block: int = 1, max_iters: int = 0,
                              horizon: int = 0, stream=None, stop: str = "block"):
