@@ -444,15 +444,19 @@ class PageMoves(NamedTuple):
     status: object
 
 
-def _on(dev, stream, launch):
+def _on(dev, stream, launch, *used):
     """launch(stream handle) with `stream` (default: the current stream of `dev`) made current, so that outputs and
-    scratch belong to it."""
+    scratch belong to it.  The tensors `used` (None: not there) are kept from reuse until a given stream has read them."""
     import torch
     if stream is not None:
         if stream.device != dev:
             raise PdError(1, f"the stream is on {stream.device}, the tensors are on {dev}")
         with torch.cuda.stream(stream):
-            return launch(stream.cuda_stream)
+            out = launch(stream.cuda_stream)
+        for t in used:
+            if t is not None:
+                t.record_stream(stream)
+        return out
     if dev.index != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):
             return launch(torch._C._cuda_getCurrentRawStream(dev.index))
@@ -525,7 +529,7 @@ def beam_select(logits, scores, lens, done, *, eos_id: int = C.EOS_ID, pad_id: i
                                 flags.data_ptr(), ws.data_ptr(), n.value, handle))
         return BeamStep(out, *ints.unbind(0), flags)
 
-    return _on(dev, stream, launch)
+    return _on(dev, stream, launch, logits, scores, lens, done, max_len)
 
 
 class PagedCache:
@@ -564,6 +568,7 @@ class PagedCache:
         self.kv_heads, self.head_dim, self.device = kv_heads, head_dim, dev
         self._c = c
         self._p = ctypes.byref(c)
+        self._buffers = self.k, self.v, self.k_scale, self.v_scale
 
     def _table(self, table, lens):
         import torch
@@ -619,7 +624,7 @@ class PagedCache:
                                      int(odt == torch.bfloat16), H * dh, None if ws is None else ws.data_ptr(), n, handle))
             return out
 
-        return _on(dev, stream, launch)
+        return _on(dev, stream, launch, *self._buffers, q, new_k, new_v, table, lens)
 
     def read(self, table, lens, first, *, layer: int = 0, count: int = 1, stream=None):
         """Values held at positions first .. first + count - 1 of each sequence, float32
@@ -637,7 +642,7 @@ class PagedCache:
                                                 first.data_ptr(), count, k.data_ptr(), v.data_ptr(), handle))
             return k, v
 
-        return _on(dev, stream, launch)
+        return _on(dev, stream, launch, *self._buffers, table, lens, first)
 
     def fork(self, table, lens, parents, *, grow: bool = True, stream=None) -> PageFork:
         """The table of the sequences whose parents are given (-1: empty), with a slot for the next token if grow
@@ -659,7 +664,7 @@ class PagedCache:
                                                 at + 4 * (n_out + self.pages), ws.data_ptr(), n, handle))
             return PageFork(new, *rest.split_with_sizes((n_out, self.pages, 2)))
 
-        return _on(dev, stream, launch)
+        return _on(dev, stream, launch, *self._buffers, table, lens, parents)
 
     def compact(self, table, lens, *, stream=None) -> PageMoves:
         """Moves the pages in use to the front of the pool (pd_pages_compact)."""
@@ -677,4 +682,4 @@ class PagedCache:
                                                    at + 4 * self.pages, ws.data_ptr(), n, handle))
             return PageMoves(new, *rest.split_with_sizes((self.pages, 2)))
 
-        return _on(dev, stream, launch)
+        return _on(dev, stream, launch, *self._buffers, table, lens)

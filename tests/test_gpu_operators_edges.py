@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2305_10427_amd import pdec
 from tests import attend_error as E, operators_ref as R
 from tests.test_gpu_operators import Pool, gpu, host, i32, say, tree_tables
 
@@ -179,3 +180,40 @@ def test_append_in_4_bits_over_floats_whole_range(dh):
         err = np.abs(got - want)
         say(name, dh, float((err / tol).max()))
         assert np.isfinite(got).all() and (err <= tol).all(), np.argwhere(~(err <= tol))[:5]
+
+
+@pytest.mark.parametrize("call", ["attend", "append", "read", "fork", "compact", "select"])
+def test_inputs_of_a_call_on_another_stream_may_be_dropped_at_once(call):
+    """The call waits on its stream; meanwhile its inputs go, and what the current stream allocates next is overwritten."""
+    g = np.random.default_rng(7)
+    S, H, dh, ps, ld = 6, 4, 64, 16, 8
+    table = g.permutation(S * ld + 20)[:S * ld].reshape(S, ld)
+    lens = [100, 64, 1, 127, 33, 90]
+
+    def inputs():
+        r = np.random.default_rng(8)
+        pool = Pool(r, "bf16", 1, S * ld + 20, ps, H, dh).cache
+        q, k, v = (gpu(r.normal(size=(S, H, dh)), torch.float32) for _ in range(3))
+        t, n, par = i32(table), i32(lens), i32([0, 0, 3, 5, -1, 1])
+        x, z, i = gpu(r.normal(size=(2, 3, 5000)), torch.float32), torch.zeros(2, 3, device="cuda"), i32(np.zeros((2, 3)))
+        return {"attend": lambda **o: pool.attend(q, t, n, **o), "append": lambda **o: pool.attend(q, t, n, new_k=k, new_v=v, **o),
+                "read": lambda **o: pool.read(t, n, n - 1 if not o else first, **o), "fork": lambda **o: pool.fork(t, n, par, **o),
+                "compact": lambda **o: pool.compact(t, n, **o), "select": lambda **o: pdec.beam_select(x, z, i, i, **o)}[call]
+
+    first = i32(lens) - 1
+    whole = lambda out: [out] if torch.is_tensor(out) else list(out)  # noqa: E731
+    want = [t.clone() for t in whole(inputs()())]
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    f = inputs()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)                         # about a tenth of a second
+    out = whole(f(stream=s))
+    del f
+    junk = [torch.full((n,), 113, dtype=torch.uint8, device="cuda") for n in [1 << 9] * 40 + [1 << 14] * 40 + [1 << 17] * 20 + [1 << 19] * 20]
+    torch.cuda.synchronize()
+    del junk
+    for a, b in zip(out, want):
+        assert torch.equal(a, b)
