@@ -228,7 +228,7 @@ class Context:
         self.handle = h
         self.B = 0
         self.device = device
-        self._beam_ws = {}
+        self._beam_ws = None
 
     def encode(self, src, src_len: Sequence[int], stream=None):
         """src: int32 device tensor [B, n_max]; src_len: host ints."""
@@ -278,8 +278,8 @@ class Context:
 
     def decode_beam(self, tgt_m: Sequence[int], beam: int = 5, alpha: float = 1.0, cache: str = "native", stream=None):
         """Beam search (pd_decode_beam): (ids [B, beam, m_max], lengths [B, beam], scores [B, beam] float32, k [B],
-        flags [B]) as device tensors, hypotheses best first.  cache: "native" (the model's type) or "int4".  The
-        workspace of a beam width and cache type is kept with the context."""
+        flags [B]) as device tensors, hypotheses best first.  cache: "native" (the model's type) or "int4".  One
+        workspace, of the most that a call has needed, is kept with the context."""
         import torch
         tgt_m = [int(x) for x in tgt_m]
         if len(tgt_m) != self.B:
@@ -288,7 +288,6 @@ class Context:
             raise PdError(1, f"unknown cache type {cache!r}")
         L = load_library()
         dt = CACHE_TYPES[self.model.cfg.dtype if cache == "native" else cache]
-        key = (int(beam), dt)
         n = ctypes.c_size_t()
         _check(L.pd_decode_beam_bytes(self.handle, int(beam), dt, ctypes.byref(n)))
         need = n.value
@@ -297,9 +296,10 @@ class Context:
         rows = max(B, 1)                     # nothing encoded: the library itself reports it
 
         def launch(handle):
-            if key not in self._beam_ws:     # here, so that it is allocated on the stream that uses it
-                self._beam_ws[key] = torch.empty(need + 256, dtype=torch.uint8, device=dev)
-            ws = self._beam_ws[key]
+            if self._beam_ws is None or self._beam_ws.numel() < need + 256:
+                self._beam_ws = None         # here, so that the new one is allocated on the stream that uses it
+                self._beam_ws = torch.empty(need + 256, dtype=torch.uint8, device=dev)
+            ws = self._beam_ws
             ws.record_stream(torch.cuda.current_stream(dev))
             ids = torch.empty((rows, beam, max(m_max, 1)), dtype=torch.int32, device=dev)
             ln = torch.empty((rows, beam), dtype=torch.int32, device=dev)
