@@ -416,6 +416,7 @@ class Context:
 
 
 # --- beam search's operators ---------------------------------------------------
+# They are for decoding: tensors that require a gradient are refused unless gradients are off.
 
 
 class BeamStep(NamedTuple):
@@ -482,6 +483,15 @@ def _tensor(name, t, dtypes, shape, dev, contiguous=True):
     return t
 
 
+def _no_gradient(**tensors):
+    """Refuses tensors that would lose a gradient: the operators have no backward pass."""
+    import torch
+    for name, t in tensors.items():
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise PdError(5, f"{name} requires a gradient, which this operator does not give: detach it, or call under "
+                             "torch.no_grad()")
+
+
 def _rows(name, t):
     """Elements from one row of a 3-D tensor to the next: the last two dimensions packed, rows of any distance."""
     if t.is_contiguous():
@@ -513,6 +523,7 @@ def beam_select(logits, scores, lens, done, *, eos_id: int = C.EOS_ID, pad_id: i
     _tensor("done", done, i32, (B, K), dev)
     if max_len is not None:
         _tensor("max_len", max_len, i32, (B,), dev)
+    _no_gradient(logits=logits, scores=scores)
     dt = 1 if logits.dtype == torch.bfloat16 else 0
     n = ctypes.c_size_t()
     _check(L.pd_beam_select_bytes(dt, B, K, V, ctypes.byref(n)))
@@ -564,6 +575,7 @@ class PagedCache:
                 x = torch.zeros(shape, dtype=dt, device=dev)
             setattr(self, name, _tensor(name, x, (dt,), shape, dev))
             setattr(c, name, x.data_ptr())
+        _no_gradient(k=k, v=v, k_scale=k_scale, v_scale=v_scale)
         self.dtype, self.layers, self.pages, self.page_size = dtype, layers, pages, page_size
         self.kv_heads, self.head_dim, self.device = kv_heads, head_dim, dev
         self._c = c
@@ -597,6 +609,7 @@ class PagedCache:
         types = (torch.float32, torch.bfloat16)
         H = q.shape[1] if len(q.shape) == 3 else None
         _tensor("q", q, types, (S, H, dh), dev, contiguous=False)
+        _no_gradient(q=q)
         odt = q.dtype if out_dtype is None else out_dtype
         if odt not in types:
             raise PdError(1, "out_dtype must be torch.float32 or torch.bfloat16")
@@ -611,6 +624,7 @@ class PagedCache:
             nld = _rows("new_k", new_k)
             if new_v.dtype != new_k.dtype or _rows("new_v", new_v) != nld:
                 raise PdError(1, "new_k and new_v must have the same type and row distance")
+            _no_gradient(new_k=new_k, new_v=new_v)
             kp, vp, ndt = new_k.data_ptr(), new_v.data_ptr(), int(new_k.dtype == torch.bfloat16)
         top = ld * self.page_size if max_len is None else max_len
         n = self._bytes("pd_cache_attend_bytes", H, S, group, top)

@@ -217,3 +217,22 @@ def test_inputs_of_a_call_on_another_stream_may_be_dropped_at_once(call):
     del junk
     for a, b in zip(out, want):
         assert torch.equal(a, b)
+
+
+def test_tensors_that_require_a_gradient_are_refused():
+    """The operators have no backward pass: a graph is never cut silently."""
+    c = pdec.PagedCache("f32", 1, 4, 16, 2, 16)
+    t, n, i = i32([[0], [1]]), i32([3, 4]), i32([[0], [0]])
+    q, k, x, z = (torch.ones(*shape, device="cuda") for shape in ((2, 4, 16), (2, 2, 16), (2, 1, 50), (2, 1)))
+    grad = lambda a: a.clone().requires_grad_()  # noqa: E731
+    calls = [lambda f: c.attend(f(q), t, n), lambda f: c.attend(q, t, n, new_k=f(k), new_v=k), lambda f: c.attend(q, t, n, new_k=k, new_v=f(k)),
+             lambda f: pdec.beam_select(f(x), z, i, i).scores, lambda f: pdec.beam_select(x, f(z), i, i).scores,
+             lambda f: pdec.PagedCache("f32", 1, 4, 16, 2, 16, k=f(c.k)).attend(q, t, n),
+             lambda f: pdec.PagedCache("f32", 1, 4, 16, 2, 16, v=f(c.v)).attend(q, t, n)]
+    for call in calls:
+        with pytest.raises(pdec.PdError) as e:
+            call(grad)
+        assert e.value.status == 5
+        with torch.no_grad():
+            a = call(grad)
+        assert torch.equal(a, call(lambda x: grad(x).detach())) and not a.requires_grad
