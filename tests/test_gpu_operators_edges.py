@@ -219,6 +219,51 @@ def test_inputs_of_a_call_on_another_stream_may_be_dropped_at_once(call):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("cache,n_in,pages", [("f32", 12, 90), ("bf16", 30, 200), ("int4", 12, 90), ("int4", 40, 8500), ("bf16", 2100, 9000)])
+def test_fork_at_page_borders_and_full_rows(cache, n_in, pages):
+    """Lengths that end a page (a fresh page), lie inside one (kept or copied), are none, or fill the table's row (refused)."""
+    g = np.random.default_rng(n_in + pages)
+    seen = {"border": 0, "inside": 0, "none": 0, "full": 0, "copied": 0, "kept": 0, "refused": 0, "grown": 0}
+    for trial in range(12 if n_in < 100 else 3):
+        ps, ld = int(g.choice([16, 64])), 4
+        lens = g.integers(0, ld, n_in) * ps
+        inside = g.random(n_in) < 0.4
+        lens[inside] = g.integers(0, ld, inside.sum()) * ps + g.integers(1, ps, inside.sum())
+        if trial % 3 == 2:
+            lens[int(g.integers(0, n_in))] = ld * ps
+        table, ids = np.full((n_in, ld), -1, np.int64), iter(g.permutation(pages))
+        for s in range(n_in):
+            for j in range(-(-int(lens[s]) // ps)):
+                share = s and g.random() < 0.5 and table[s - 1, j] >= 0 and (j < lens[s] // ps) == (j < lens[s - 1] // ps)
+                table[s, j] = table[s - 1, j] if share else next(ids, -1)
+        parents = g.integers(0, n_in, n_in)
+        parents[:n_in // 4] = -1                               # finished hypotheses
+        if trial % 3 == 2:
+            parents[-1] = int(np.argmax(lens))
+        pool = Pool(g, cache, 2, pages, ps, 1, 16)
+        before = {n: t.clone() for n, t in pool.tensors().items()}
+        r = pool.cache.fork(i32(table), i32(lens), i32(parents))
+        new, ln, refs, st, cp = R.fork(table, lens, parents, pages, ps, True)
+        for got, want in ((r.table, new), (r.lens, ln), (r.refs, refs)):
+            np.testing.assert_array_equal(host(got), want)
+        assert r.status.tolist() == st
+        for n, t in before.items():
+            for a, b in cp:
+                t[:, b] = t[:, a]
+            assert torch.equal(t, pool.tensors()[n])
+        n = lens[parents[parents >= 0]]
+        seen["full"] += int((n == ld * ps).sum())
+        seen["none"] += int((n == 0).sum())
+        seen["border"] += int(((n % ps == 0) & (n > 0) & (n < ld * ps)).sum())
+        seen["inside"] += int((n % ps > 0).sum())
+        seen["refused"] += st[0] > 0
+        seen["grown"] += st[0] == 0
+        seen["copied"] += len(cp)
+        seen["kept"] += int((n % ps > 0).sum()) - len(cp) if st[0] == 0 else 0
+    say(cache, n_in, pages, seen)
+    assert min(seen.values()) > 0
+
+
 def test_tensors_that_require_a_gradient_are_refused():
     """The operators have no backward pass: a graph is never cut silently."""
     c = pdec.PagedCache("f32", 1, 4, 16, 2, 16)
