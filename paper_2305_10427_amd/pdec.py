@@ -483,6 +483,12 @@ def _tensor(name, t, dtypes, shape, dev, contiguous=True):
     return t
 
 
+def _shape(t, dims):
+    """A tensor's own shape, or that of any tensor of `dims` dimensions where it is not one (_tensor then refuses it)."""
+    shape = getattr(t, "shape", ())
+    return shape if len(shape) == dims else (None,) * dims
+
+
 def _no_gradient(**tensors):
     """Refuses tensors that would lose a gradient: the operators have no backward pass."""
     import torch
@@ -512,7 +518,7 @@ def beam_select(logits, scores, lens, done, *, eos_id: int = C.EOS_ID, pad_id: i
         raise PdError(1, "scores must be a tensor")
     dev = scores.device
     f32, i32 = (torch.float32,), (torch.int32,)
-    shape = logits.shape if isinstance(logits, torch.Tensor) and logits.dim() == 3 else (None, None, None)
+    shape = _shape(logits, 3)
     _tensor("logits", logits, (torch.float32, torch.bfloat16), shape, dev, contiguous=False)
     B, K, V = shape
     ld = logits.stride(1) if K > 1 else logits.stride(0) if B > 1 else V
@@ -585,9 +591,7 @@ class PagedCache:
     def _table(self, table, lens):
         import torch
         i32 = (torch.int32,)
-        shape = table.shape
-        if len(shape) != 2:
-            _tensor("table", table, i32, (None, None), self.device)
+        shape = _shape(table, 2)
         _tensor("table", table, i32, shape, self.device)
         _tensor("lens", lens, i32, shape[:1], self.device)
         return shape
@@ -607,7 +611,7 @@ class PagedCache:
         S, ld = self._table(table, lens)
         dev, dh = self.device, self.head_dim
         types = (torch.float32, torch.bfloat16)
-        H = q.shape[1] if len(q.shape) == 3 else None
+        H = _shape(q, 3)[1]
         _tensor("q", q, types, (S, H, dh), dev, contiguous=False)
         _no_gradient(q=q)
         odt = q.dtype if out_dtype is None else out_dtype
@@ -664,7 +668,7 @@ class PagedCache:
         import torch
         S, ld = self._table(table, lens)
         dev = self.device
-        _tensor("parents", parents, (torch.int32,), parents.shape if len(parents.shape) == 1 else (None,), dev)
+        _tensor("parents", parents, (torch.int32,), _shape(parents, 1), dev)
         n_out = parents.shape[0]
         n = self._bytes("pd_pages_bytes", n_out)
 

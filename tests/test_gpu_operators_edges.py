@@ -281,3 +281,16 @@ def test_tensors_that_require_a_gradient_are_refused():
         with torch.no_grad():
             a = call(grad)
         assert torch.equal(a, call(lambda x: grad(x).detach())) and not a.requires_grad
+
+
+def test_arguments_that_are_no_tensors_are_refused():
+    c = pdec.PagedCache("bf16", 1, 4, 16, 2, 16)
+    t, n, q, k = i32([[0], [1]]), i32([3, 4]), torch.ones(2, 4, 16, device="cuda"), torch.ones(2, 2, 16, device="cuda")
+    x, z, i = torch.ones(2, 1, 50, device="cuda"), torch.ones(2, 1, device="cuda"), i32([[0], [0]])
+    for bad in (None, [[0], [1]], np.zeros((2, 1), np.int32), 3.0):
+        for call in (lambda: c.attend(bad, t, n), lambda: c.attend(q, bad, n), lambda: c.attend(q, t, bad), lambda: c.fork(t, n, bad),
+                     lambda: c.fork(bad, n, n), lambda: c.compact(bad, n), lambda: c.compact(t, bad), lambda: c.read(t, n, bad),
+                     lambda: c.read(bad, n, n), lambda: pdec.beam_select(bad, z, i, i), lambda: pdec.beam_select(x, bad, i, i),
+                     lambda: pdec.beam_select(x, z, bad, i), lambda: pdec.beam_select(x, z, i, bad), lambda: c.attend(q, t, n, new_k=k, new_v=[1])):
+            with pytest.raises(pdec.PdError):
+                call()
