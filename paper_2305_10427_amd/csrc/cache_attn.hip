@@ -421,7 +421,10 @@ template <int CT> constexpr int kSegLane = CT == CT_F32 ? 32 : CT == CT_BF16 ? 1
 
 // Split of the launch: beams per tile, tiles of a group, parts of the keys.
 // Part z takes units z, z + splits, ...: behind the beams' common prefix a block
-// has an item for each of them, and every part gets its share of those.
+// has an item for each of them, and units in turn spread those over the parts.
+// Evenly only where there are many more of them than parts: 2 x 4 rows of 20,011 ..
+// 32,749 keys, nine tenths in common, have 16 to 26 such units for 64 parts, so a
+// wave has 4.2 items on average and 7 at most.
 struct Plan {
   int rows_per_tile, tiles, splits;
 };
@@ -435,14 +438,16 @@ constexpr int waves_per_simd(int ct, int dh) {
 }
 
 // Long caches are bound by memory in float32 and bfloat16 (16 rows of 8,191 ..
-// 16,381 keys, 16 heads of 64, bfloat16, 805 MB: 150 us, 5.4 TB/s; reading alone
-// reaches 5.9) and by the vector instructions that unpack in 4 bits (2 x 4 rows of
-// 20,011 .. 32,749 keys, 4 heads of 128 for 16, 44 MB, float output: 30.5 us; 64 x 4 rows of 4,000
-// keys of 64, 312 MB: 124 us, 2.5 TB/s).  Short ones are a chain of latencies -
-// lengths, table, keys, products, the waves' join - of 6 us for one sentence and,
-// with 512 workgroups (64 x 5 rows of 15 .. 138 keys, 8 heads, bfloat16, 29 MB),
-// 15.4 us, of which the append is 1.7: its stores have to land before its keys are
-// read.
+// 16,381 keys, 16 heads of 64, bfloat16, 805 MB: 151 us, 5.3 TB/s; 8 heads of 64 in
+// float32: 154 us, 5.2; reading alone reaches 5.9).  In 4 bits (64 x 4 rows of 4,000
+// keys of 64, 312 MB: 124 us, 2.5 TB/s; 2 x 4 rows of 20,011 .. 32,749 keys, 4 heads
+// of 128 for 16, 44 MB: 30.6 us) a wave issues vector instructions, which unpack
+// codes and split weights, 38% of its time and waits 35%, and waves have unequal
+// work.  Short ones are a chain of latencies - lengths, table, keys, products, the
+// waves' join - of 6 us for one sentence.  With 512 workgroups (64 x 5 rows of 15 ..
+// 138 keys, 8 heads, bfloat16, 29 MB) they take 16.3 us: the longest sentence's
+// busiest wave has 5 items, one requested ahead, and waits 54% of its time; 1.6 of it
+// is the append, whose stores have to land before its keys are read.
 //
 // Weights enter the product with V in three bfloat16 parts, float's own 2^-24,
 // whatever the output's type: with two (2^-17) 1.0e-3 to 1.7e-3 of the bfloat16
@@ -955,12 +960,13 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
 namespace {
 
 // Beams per tile: whole beams within 16 query rows.  Parts of the keys: as many
-// as the chip holds workgroups at once, a second round of workgroups costing
-// more than it evens out (64 x 4 rows of 4,000 keys, 64 wide: bfloat16 73 us with
-// 768 workgroups, 103 with 1,024; 4 bits 55 and 71); but one below kSplitUnits
-// units, where joining the parts costs more than the workgroup's longer way (5
-// rows of 8 heads, bfloat16, one part / parts of a unit and their join: 138 keys
-// 9.5 / 11.6 us, 300 12.2 / 12.7, 600 17.1 / 14.0, 1,024 24.5 / 14.9).
+// whole ones as the chip holds workgroups at once, a second round of workgroups
+// costing more than it evens out (64 x 4 rows of 4,000 keys, 4 heads of 64: bfloat16
+// 94 us with 768 workgroups, 105 with 1,024; 4 bits 64 and 69); but one below
+// kSplitUnits units, where joining the parts costs about what the workgroup's longer
+// way does (5 rows of 8 heads, bfloat16, one part / parts of a unit and their join:
+// 138 keys 9.2 / 9.9 us, 300 12.3 / 11.2, 600 17.9 / 12.4, 1,024 26.3 / 13.1; with the
+// host's part of two launches 300 keys 12.2 / 12.7).
 constexpr int kCus = 256;
 constexpr int kSplitUnits = 4;
 Plan plan_attend(const CacheView& c, int n_seqs, int heads, int group, int max_len) {
