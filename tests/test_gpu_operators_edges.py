@@ -219,6 +219,34 @@ def test_inputs_of_a_call_on_another_stream_may_be_dropped_at_once(call):
         assert torch.equal(a, b)
 
 
+def test_calls_on_a_given_stream_can_be_captured():
+    """Captured on a stream that the calls are given too; every replay equals the eager calls made between them."""
+    g = np.random.default_rng(51)
+    pool = Pool(g, "int4", 1, 64, 16, 4, 64).cache
+    t, n = i32(np.arange(60).reshape(4, 15)), i32([200, 100, 50, 180])
+    q = gpu(g.normal(size=(4, 8, 64)), torch.float32)
+    x, z, i = gpu(3 * g.normal(size=(4, 1, 40001)), torch.float32), torch.zeros(4, 1, device="cuda"), i32(np.zeros((4, 1)))
+    s = torch.cuda.Stream()
+
+    def run(**o):
+        return (pool.attend(q * 0.5, t, n, **o), *pdec.beam_select(x, z, i, i, **o), *pool.fork(t, n, i[:, 0] + 1, grow=False, **o),
+                *pool.read(t, n, n - 1, **o))
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        out = run(stream=s)
+    for k in range(4):
+        q.copy_(gpu(g.normal(size=(4, 8, 64)), torch.float32))
+        x.mul_(-0.9)
+        want = run()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), k
+
+
 @pytest.mark.parametrize("cache,n_in,pages", [("f32", 12, 90), ("bf16", 30, 200), ("int4", 12, 90), ("int4", 40, 8500), ("bf16", 2100, 9000)])
 def test_fork_at_page_borders_and_full_rows(cache, n_in, pages):
     """Lengths that end a page (a fresh page), lie inside one (kept or copied), are none, or fill the table's row (refused)."""
